@@ -744,6 +744,114 @@ int fesc_calib_valu(fesc_ctx* ctx, int kind, uint32_t iters, double* rate, void*
 #define FESC_CALIB_HBM_COPY 1
 int fesc_calib_hbm(fesc_ctx* ctx, int kind, size_t bytes, double* rate, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The block in the clear.  The same computations that the calls above carry
+ * under encryption (the affine scan and its contraction, Eq.
+ * "hescan-contract-output"; skip connection, gate and norm of the post-SSM
+ * path), on unencrypted activations and with their gradients: for the model
+ * whose weights are packed (its training, the ranges that fix scales and the
+ * conversion bound), for the answers that decrypted outputs are held against,
+ * and for traffic that needs no encryption.
+ *
+ * These calls need no context.  `dtype` is the type of every activation,
+ * weight and gradient of a call (FESC_F32, FESC_BF16); states are fp32 in
+ * either case, as are all sums.  Strides count elements.  A workspace is a
+ * device buffer of the caller, aligned to 16 bytes, of at least the size that
+ * the matching query returns (it may be NULL where that is 0); its contents
+ * mean nothing between calls.  Outputs must not overlap inputs, except a
+ * state that a call names as updated in place.  Results do not depend on the
+ * order of execution (no atomics).  No call allocates, waits or copies to the
+ * host; all may be captured into a graph.  Values that are not finite make the
+ * outputs of their own sequence (row, in the norms) undefined, no others.
+ * ------------------------------------------------------------------------ */
+#define FESC_F32 0
+#define FESC_BF16 1
+
+/* Gated linear recurrence.  Per sequence and head h (group g = h / (heads /
+ * groups)), with the factors of the paper's packet x_t in R^P, a_t, B_t, C_t
+ * in R^N (P = head_dim, N = d_state) and a_t = exp(la_t):
+ *     S_t = a_t S_{t-1} + x_t B_t^T,     y_t = S_t C_t,     S_0 = h0 or 0.
+ * la <= 0; la = -inf (a_t = 0) forgets what came before exactly, so several
+ * documents may follow each other in one row.  Layouts (the last dimensions
+ * contiguous; token and batch strides are free, so factors may be slices of
+ * one wider array): x [batch][len][heads][head_dim], la [batch][len][heads],
+ * B and C [batch][len][groups][d_state]; dy like x.  y, dx, dla, db and dc
+ * are contiguous; states are contiguous float [batch][heads][head_dim][d_state].
+ * 1 <= d_state <= 128, 1 <= head_dim <= 4096, heads <= 4096 and a multiple of
+ * groups.  batch or len may be 0. */
+typedef struct fesc_clear_scan_desc {
+  uint32_t dtype;
+  uint32_t batch, len;
+  uint32_t heads, head_dim, groups, d_state;
+  uint64_t x_token, x_batch;
+  uint64_t la_token, la_batch;
+  uint64_t b_token, b_batch;
+  uint64_t c_token, c_batch;
+  uint64_t dy_token, dy_batch; /* backward only */
+} fesc_clear_scan_desc;
+
+/* Bytes of workspace of the forward (backward = 0) or backward call. */
+int fesc_clear_scan_workspace(const fesc_clear_scan_desc* desc, int backward, size_t* bytes);
+
+/* y and, unless NULL, the final state hT.  h0 may be NULL (zero). */
+int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* x, const void* la, const void* B,
+                    const void* C, const float* h0, void* y, float* hT, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* Gradients of a loss whose gradients are dy and dhT (NULL: zero).  dh0 may
+ * be NULL (not wanted).  dla is the gradient of la (0 where la = -inf); db and
+ * dc sum over the heads of their group. */
+int fesc_clear_scan_bwd(const fesc_clear_scan_desc* desc, const void* x, const void* la,
+                        const void* B, const void* C, const float* h0, const void* dy,
+                        const float* dhT, void* dx, void* dla, void* db, void* dc, float* dh0,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token of each of `batch` rows: the recurrence's step on a pool of states
+ * float [pool][heads][head_dim][d_state], in place.  Row i uses state slots[i]
+ * (NULL: i, and pool >= batch).  A slot outside [0, pool) marks an idle row:
+ * its y is zero and no state is touched.  No two rows may name one slot.  Of
+ * the descriptor, len and the token strides are not used; y is
+ * [batch][heads][head_dim]. */
+int fesc_clear_scan_step(const fesc_clear_scan_desc* desc, const void* x, const void* la,
+                         const void* B, const void* C, float* state, uint32_t pool,
+                         const int32_t* slots, void* y, void* stream);
+
+/* Norms over rows of `width` channels (1 <= width <= 16384), each fused with
+ * what stands before it in the block.  Rows of inputs start row strides
+ * apart; outputs and weight vectors are contiguous.  eps > 0.
+ *   gated:    v = (m + skip x) silu(z),   u = v w / sqrt(mean v^2 + eps)
+ *   residual: v = r + scale o,            u as above; r_new = v is returned
+ * skip, scale and w are vectors of `width`. */
+typedef struct fesc_clear_norm_desc {
+  uint32_t dtype;
+  uint32_t width;
+  uint64_t rows;
+  float eps;
+  uint64_t m_row, x_row, z_row; /* gated */
+  uint64_t o_row, r_row;        /* residual */
+  uint64_t du_row, dr_row;      /* backward: du; dr_new */
+} fesc_clear_norm_desc;
+
+int fesc_clear_norm_gated(const fesc_clear_norm_desc* desc, const void* m, const void* x,
+                          const void* z, const void* skip, const void* w, void* u, void* stream);
+int fesc_clear_norm_residual(const fesc_clear_norm_desc* desc, const void* o, const void* r,
+                             const void* scale, const void* w, void* r_new, void* u,
+                             void* stream);
+
+/* Bytes of workspace of either backward call. */
+int fesc_clear_norm_workspace(const fesc_clear_norm_desc* desc, size_t* bytes);
+
+/* Gradients.  residual: d_o is the gradient of o, dr that of r; du or dr_new
+ * may be NULL (zero). */
+int fesc_clear_norm_gated_bwd(const fesc_clear_norm_desc* desc, const void* m, const void* x,
+                              const void* z, const void* skip, const void* w, const void* du,
+                              void* dm, void* dx, void* dz, void* dskip, void* dw,
+                              void* workspace, size_t workspace_bytes, void* stream);
+int fesc_clear_norm_residual_bwd(const fesc_clear_norm_desc* desc, const void* o, const void* r,
+                                 const void* scale, const void* w, const void* du,
+                                 const void* dr_new, void* d_o, void* dr, void* dscale, void* dw,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,408 @@
+// C entry points of the block in the clear: argument checks, workspace
+// layout, and the rules that split the work (kernels: clear_scan.hip,
+// clear_norm.hip).
+#include "clear.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+#include "fesc_internal.hpp"
+
+using namespace fesc;
+
+namespace {
+
+hipStream_t S(void* stream) { return reinterpret_cast<hipStream_t>(stream); }
+
+constexpr uint64_t kMaxStride = 1ull << 40;
+// A launch counts its work items in 32 bits.
+constexpr uint64_t kMaxGrid256 = 1ull << 24, kMaxGrid512 = 1ull << 23;
+
+uint32_t elem_bytes(uint32_t dtype) { return dtype == FESC_BF16 ? 2 : 4; }
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+int check_scan(const fesc_clear_scan_desc* d) {
+  if (!d) return fail(FESC_ERR_ARG, "null descriptor");
+  if (d->dtype != FESC_F32 && d->dtype != FESC_BF16)
+    return fail(FESC_ERR_ARG, "dtype: float32 or bfloat16");
+  if (d->heads == 0 || d->heads > 4096 || d->groups == 0 || d->heads % d->groups)
+    return fail(FESC_ERR_ARG, "heads: 1..4096 and a multiple of groups");
+  if (d->head_dim == 0 || d->head_dim > 4096) return fail(FESC_ERR_ARG, "head_dim: 1..4096");
+  if (d->d_state == 0 || d->d_state > kMaxState) return fail(FESC_ERR_ARG, "d_state: 1..128");
+  for (uint64_t s : {d->x_token, d->x_batch, d->la_token, d->la_batch, d->b_token, d->b_batch,
+                     d->c_token, d->c_batch, d->dy_token, d->dy_batch})
+    if (s > kMaxStride) return fail(FESC_ERR_ARG, "stride too large");
+  return FESC_OK;
+}
+
+// Rows of 16 bytes: base and strides, in elements, are multiples of them.
+struct Rows {
+  uint32_t per;  // elements in 16 bytes
+  bool ok = true;
+  explicit Rows(uint32_t dtype) : per(16 / elem_bytes(dtype)) {}
+  Rows& add(const void* p, uint64_t s0, uint64_t s1 = 0) {
+    ok = ok && aligned(p, 16) && s0 % per == 0 && s1 % per == 0;
+    return *this;
+  }
+  Rows& len(uint64_t n) {
+    ok = ok && n % per == 0;
+    return *this;
+  }
+};
+
+// Workgroups that a state pass should have: two for each of 256 compute units.
+constexpr uint64_t kWantedGroups = 512;
+
+// A workgroup carries one head's state (a tile of 64 channels) from chunk to
+// chunk.  Where there are too few heads to fill the chip the sequence is cut
+// into segments of whole chunks, two at least (a segment's pass over its own
+// tokens is the price: x and B are read twice).
+ScanShape shape_of(const fesc_clear_scan_desc* d) {
+  ScanShape s{};
+  s.batch = d->batch;
+  s.len = d->len;
+  s.heads = d->heads;
+  s.head_dim = d->head_dim;
+  s.groups = d->groups;
+  s.d_state = d->d_state;
+  s.la_token = d->la_token;
+  s.la_batch = d->la_batch;
+  s.chunks = (uint32_t)(((uint64_t)d->len + kChunk - 1) / kChunk);
+  s.ptiles = (d->head_dim + kPTile - 1) / kPTile;
+  const uint64_t groups = (uint64_t)d->batch * d->heads * s.ptiles;
+  const uint64_t want = std::max<uint64_t>(1, groups ? kWantedGroups / groups : 1);
+  const uint64_t segs = std::min<uint64_t>(want, std::max<uint32_t>(1, s.chunks / 2));
+  s.seg_chunks = (uint32_t)((s.chunks + segs - 1) / segs);
+  s.segs = s.chunks ? (s.chunks + s.seg_chunks - 1) / s.seg_chunks : 1;
+  return s;
+}
+
+// Heads of a group in turn in one workgroup of the gradient kernel; split
+// over workgroups where chunks alone are too few.
+void split_heads(const ScanShape& s, uint32_t* splits, uint32_t* per) {
+  const uint32_t heads = s.heads / s.groups;
+  const uint64_t groups = (uint64_t)s.batch * s.chunks * s.groups;
+  const uint64_t want = std::min<uint64_t>(heads, groups ? (256 + groups - 1) / groups : 1);
+  *per = (uint32_t)((heads + want - 1) / want);
+  *splits = (heads + *per - 1) / *per;
+}
+
+uint64_t state_count(const ScanShape& s) {
+  return (uint64_t)s.batch * s.heads * s.head_dim * s.d_state;
+}
+
+// The workspace, laid out or only measured (base null).
+struct Space {
+  char* base;
+  size_t used = 0;
+  explicit Space(void* p) : base((char*)p) {}
+  template <typename T>
+  T* take(uint64_t count, size_t bytes = sizeof(T)) {
+    char* p = base ? base + used : nullptr;
+    used += round_up(count * bytes);
+    return reinterpret_cast<T*>(p);
+  }
+};
+
+void seg_space(Space& w, const ScanShape& s, ScanDir* d) {
+  if (s.segs == 1) return;
+  d->seg_states = w.take<float>(state_count(s) * s.segs);
+  d->seg_decay = w.take<float>((uint64_t)s.batch * s.heads * s.segs);
+}
+
+void grad_space(Space& w, const ScanShape& s, uint32_t dtype, ScanDir* dir, ScanGrad* g) {
+  for (int k = 0; k < 2; ++k) {
+    seg_space(w, s, dir + k);
+    dir[k].chunk_states = w.take<char>(state_count(s) * s.chunks, elem_bytes(dtype));
+  }
+  split_heads(s, &g->splits, &g->heads_per_split);
+  if (g->splits > 1) {
+    const uint64_t n = (uint64_t)s.batch * s.len * s.groups * s.d_state * g->splits;
+    g->db_part = w.take<float>(n);
+    g->dc_part = w.take<float>(n);
+  }
+}
+
+int check_grid(const ScanShape& s) {
+  const uint64_t bh = (uint64_t)s.batch * s.heads;
+  const uint64_t join = ((uint64_t)s.head_dim * s.d_state + 255) / 256;
+  if (bh * s.ptiles * s.segs >= kMaxGrid256 || bh * join >= kMaxGrid256 ||
+      (uint64_t)s.batch * s.chunks >= kMaxGrid512 ||
+      (uint64_t)s.batch * s.len * s.groups * s.d_state >= kMaxGrid256 * 256)
+    return fail(FESC_ERR_ARG, "batch * len * heads too large for one call");
+  return FESC_OK;
+}
+
+int check_workspace(const void* p, size_t have, size_t need) {
+  if (have < need) return fail(FESC_ERR_ARG, "workspace too small");
+  if (need && !p) return fail(FESC_ERR_ARG, "null workspace");
+  if (!aligned(p, 16)) return fail(FESC_ERR_ARG, "workspace: not aligned to 16 bytes");
+  return FESC_OK;
+}
+
+bool word_groups(const ScanShape& s, uint32_t dtype, const void* p) {
+  return s.head_dim % 4 == 0 && aligned(p, 4 * elem_bytes(dtype));
+}
+
+int check_norm(const fesc_clear_norm_desc* d) {
+  if (!d) return fail(FESC_ERR_ARG, "null descriptor");
+  if (d->dtype != FESC_F32 && d->dtype != FESC_BF16)
+    return fail(FESC_ERR_ARG, "dtype: float32 or bfloat16");
+  if (d->width == 0 || d->width > 16384) return fail(FESC_ERR_ARG, "width: 1..16384");
+  if (!(d->eps > 0.0f) || !std::isfinite(d->eps)) return fail(FESC_ERR_ARG, "eps: positive");
+  for (uint64_t s : {d->m_row, d->x_row, d->z_row, d->o_row, d->r_row, d->du_row, d->dr_row})
+    if (s > kMaxStride) return fail(FESC_ERR_ARG, "stride too large");
+  if (d->rows > 1ull << 40) return fail(FESC_ERR_ARG, "rows: at most 2^40");
+  return FESC_OK;
+}
+
+NormArgs norm_args(const fesc_clear_norm_desc* d, bool gated, const void* a, const void* b,
+                   const void* c, const void* k, const void* w) {
+  NormArgs n{};
+  n.rows = d->rows;
+  n.width = d->width;
+  n.eps = d->eps;
+  n.a = a;
+  n.b = b;
+  n.c = c;
+  n.k = k;
+  n.w = w;
+  n.a_row = gated ? d->m_row : d->o_row;
+  n.b_row = gated ? d->x_row : d->r_row;
+  n.c_row = gated ? d->z_row : 0;
+  n.du_row = d->du_row;
+  n.dr_row = d->dr_row;
+  return n;
+}
+
+bool norm_vec(const fesc_clear_norm_desc* d, const NormArgs& n) {
+  Rows r(d->dtype);
+  // a lane's unit is 8 channels in either type
+  return d->width % 8 == 0 && r.add(n.a, n.a_row).add(n.b, n.b_row).add(n.c, n.c_row)
+      .add(n.k, 0).add(n.w, 0).add(n.u, 0).add(n.r_new, 0).add(n.du, n.du ? n.du_row : 0)
+      .add(n.dr_new, n.dr_new ? n.dr_row : 0).add(n.da, 0).add(n.db, 0).add(n.dc, 0).ok;
+}
+
+int norm_bwd(const fesc_clear_norm_desc* d, bool gated, NormArgs n, void* workspace,
+             size_t workspace_bytes, void* stream) {
+  size_t need;
+  if (int rc = fesc_clear_norm_workspace(d, &need)) return rc;
+  if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
+  n.part = reinterpret_cast<float*>(workspace);
+  n.blocks = norm_grad_blocks(n.rows, n.width);
+  n.vec = norm_vec(d, n);
+  return hip_check(launch_norm_grad(d->dtype, gated, n, S(stream)), "norm gradient");
+}
+
+}  // namespace
+
+extern "C" {
+
+int fesc_clear_scan_workspace(const fesc_clear_scan_desc* d, int backward, size_t* bytes) {
+  if (int rc = check_scan(d)) return rc;
+  if (!bytes) return fail(FESC_ERR_ARG, "null argument");
+  const ScanShape s = shape_of(d);
+  Space w(nullptr);
+  ScanDir dir[2] = {};
+  ScanGrad g{};
+  if (backward)
+    grad_space(w, s, d->dtype, dir, &g);
+  else
+    seg_space(w, s, dir);
+  *bytes = w.used;
+  return FESC_OK;
+}
+
+int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la, const void* B,
+                    const void* C, const float* h0, void* y, float* hT, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+  if (int rc = check_scan(d)) return rc;
+  ScanShape s = shape_of(d);
+  if (int rc = check_grid(s)) return rc;
+  if (d->batch == 0) return FESC_OK;
+  if (d->len == 0)
+    return hT ? hip_check(launch_state_copy(h0, hT, state_count(s), S(stream)), "scan") : FESC_OK;
+  if (!x || !la || !B || !C || !y) return fail(FESC_ERR_ARG, "null buffer");
+  ScanDir dir{};
+  Space w(workspace);
+  seg_space(w, s, &dir);
+  if (int rc = check_workspace(workspace, workspace_bytes, w.used)) return rc;
+  s.la = la;
+  s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
+              .add(C, d->c_token, d->c_batch).len(d->head_dim).len(d->d_state).ok;
+  s.st4 = d->d_state % 4 == 0 && aligned(h0, 16) && aligned(hT, 16);
+  s.ch4 = word_groups(s, d->dtype, y);
+  dir.u = x;
+  dir.v = B;
+  dir.u_token = d->x_token;
+  dir.u_batch = d->x_batch;
+  dir.v_token = d->b_token;
+  dir.v_batch = d->b_batch;
+  dir.init = h0;
+  dir.fin = hT;
+  const ScanOut out{C, (int64_t)d->c_token, (int64_t)d->c_batch, y};
+  return hip_check(launch_scan_out(d->dtype, s, dir, out, S(stream)), "scan");
+}
+
+int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void* la,
+                        const void* B, const void* C, const float* h0, const void* dy,
+                        const float* dhT, void* dx, void* dla, void* db, void* dc, float* dh0,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_scan(d)) return rc;
+  ScanShape s = shape_of(d);
+  if (int rc = check_grid(s)) return rc;
+  if (d->batch == 0) return FESC_OK;
+  if (d->len == 0)
+    return dh0 ? hip_check(launch_state_copy(dhT, dh0, state_count(s), S(stream)), "scan gradient")
+               : FESC_OK;
+  if (!x || !la || !B || !C || !dy || !dx || !dla || !db || !dc)
+    return fail(FESC_ERR_ARG, "null buffer");
+  ScanDir dir[2] = {};
+  ScanGrad g{};
+  Space w(workspace);
+  grad_space(w, s, d->dtype, dir, &g);
+  if (int rc = check_workspace(workspace, workspace_bytes, w.used)) return rc;
+  s.la = la;
+  s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
+              .add(C, d->c_token, d->c_batch).add(dy, d->dy_token, d->dy_batch).len(d->head_dim)
+              .len(d->d_state).ok;
+  s.st4 = d->d_state % 4 == 0 && aligned(h0, 16) && aligned(dhT, 16) && aligned(dh0, 16) &&
+          aligned(db, 16) && aligned(dc, 16);
+  s.ch4 = word_groups(s, d->dtype, dx);
+  dir[0].u = x;
+  dir[0].v = B;
+  dir[0].u_token = d->x_token;
+  dir[0].u_batch = d->x_batch;
+  dir[0].v_token = d->b_token;
+  dir[0].v_batch = d->b_batch;
+  dir[0].init = h0;
+  dir[1].u = dy;
+  dir[1].v = C;
+  dir[1].u_token = d->dy_token;
+  dir[1].u_batch = d->dy_batch;
+  dir[1].v_token = d->c_token;
+  dir[1].v_batch = d->c_batch;
+  dir[1].init = dhT;
+  dir[1].fin = dh0;
+  dir[1].reverse = true;
+  if (int rc = hip_check(launch_scan_states(d->dtype, s, dir, 2, S(stream)), "scan gradient"))
+    return rc;
+  g.x = x;
+  g.b = B;
+  g.c = C;
+  g.dy = dy;
+  g.x_token = d->x_token;
+  g.x_batch = d->x_batch;
+  g.b_token = d->b_token;
+  g.b_batch = d->b_batch;
+  g.c_token = d->c_token;
+  g.c_batch = d->c_batch;
+  g.dy_token = d->dy_token;
+  g.dy_batch = d->dy_batch;
+  g.s_in = dir[0].chunk_states;
+  g.r_in = dir[1].chunk_states;
+  g.dx = dx;
+  g.dla = dla;
+  g.db = db;
+  g.dc = dc;
+  return hip_check(launch_scan_grad(d->dtype, s, g, S(stream)), "scan gradient");
+}
+
+int fesc_clear_scan_step(const fesc_clear_scan_desc* d, const void* x, const void* la,
+                         const void* B, const void* C, float* state, uint32_t pool,
+                         const int32_t* slots, void* y, void* stream) {
+  if (int rc = check_scan(d)) return rc;
+  if ((uint64_t)d->batch * d->heads >= kMaxGrid256)
+    return fail(FESC_ERR_ARG, "batch * heads too large for one call");
+  if (!slots && pool < d->batch) return fail(FESC_ERR_ARG, "pool: fewer states than rows");
+  if (d->batch == 0) return FESC_OK;
+  if (!x || !la || !B || !C || !y || (!state && pool)) return fail(FESC_ERR_ARG, "null buffer");
+  StepArgs a{};
+  a.x = x;
+  a.la = la;
+  a.b = B;
+  a.c = C;
+  a.x_row = d->x_batch;
+  a.la_row = d->la_batch;
+  a.b_row = d->b_batch;
+  a.c_row = d->c_batch;
+  a.state = state;
+  a.slots = slots;
+  a.y = y;
+  a.rows = d->batch;
+  a.pool = pool;
+  a.heads = d->heads;
+  a.head_dim = d->head_dim;
+  a.groups = d->groups;
+  a.d_state = d->d_state;
+  a.st4 = d->d_state % 4 == 0 && aligned(state, 16);
+  return hip_check(launch_scan_step(d->dtype, a, S(stream)), "scan step");
+}
+
+int fesc_clear_norm_gated(const fesc_clear_norm_desc* d, const void* m, const void* x,
+                          const void* z, const void* skip, const void* w, void* u, void* stream) {
+  if (int rc = check_norm(d)) return rc;
+  if (d->rows == 0) return FESC_OK;
+  if (!m || !x || !z || !skip || !w || !u) return fail(FESC_ERR_ARG, "null buffer");
+  NormArgs n = norm_args(d, true, m, x, z, skip, w);
+  n.u = u;
+  n.vec = norm_vec(d, n);
+  return hip_check(launch_norm(d->dtype, true, n, S(stream)), "gated norm");
+}
+
+int fesc_clear_norm_residual(const fesc_clear_norm_desc* d, const void* o, const void* r,
+                             const void* scale, const void* w, void* r_new, void* u,
+                             void* stream) {
+  if (int rc = check_norm(d)) return rc;
+  if (d->rows == 0) return FESC_OK;
+  if (!o || !r || !scale || !w || !r_new || !u) return fail(FESC_ERR_ARG, "null buffer");
+  NormArgs n = norm_args(d, false, o, r, nullptr, scale, w);
+  n.u = u;
+  n.r_new = r_new;
+  n.vec = norm_vec(d, n);
+  return hip_check(launch_norm(d->dtype, false, n, S(stream)), "residual norm");
+}
+
+int fesc_clear_norm_workspace(const fesc_clear_norm_desc* d, size_t* bytes) {
+  if (int rc = check_norm(d)) return rc;
+  if (!bytes) return fail(FESC_ERR_ARG, "null argument");
+  *bytes = round_up((size_t)norm_grad_blocks(d->rows, d->width) * 2 * d->width * sizeof(float));
+  return FESC_OK;
+}
+
+int fesc_clear_norm_gated_bwd(const fesc_clear_norm_desc* d, const void* m, const void* x,
+                              const void* z, const void* skip, const void* w, const void* du,
+                              void* dm, void* dx, void* dz, void* dskip, void* dw,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_norm(d)) return rc;
+  if (!skip || !w || !dskip || !dw || (d->rows && (!m || !x || !z || !du || !dm || !dx || !dz)))
+    return fail(FESC_ERR_ARG, "null buffer");
+  NormArgs n = norm_args(d, true, m, x, z, skip, w);
+  n.du = du;
+  n.da = dm;
+  n.db = dx;
+  n.dc = dz;
+  n.dk = dskip;
+  n.dw = dw;
+  return norm_bwd(d, true, n, workspace, workspace_bytes, stream);
+}
+
+int fesc_clear_norm_residual_bwd(const fesc_clear_norm_desc* d, const void* o, const void* r,
+                                 const void* scale, const void* w, const void* du,
+                                 const void* dr_new, void* d_o, void* dr, void* dscale, void* dw,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_norm(d)) return rc;
+  if (!scale || !w || !dscale || !dw || (d->rows && (!o || !r || !d_o || !dr)))
+    return fail(FESC_ERR_ARG, "null buffer");
+  NormArgs n = norm_args(d, false, o, r, nullptr, scale, w);
+  n.du = du;
+  n.dr_new = dr_new;
+  n.da = d_o;
+  n.db = dr;
+  n.dk = dscale;
+  n.dw = dw;
+  return norm_bwd(d, false, n, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,101 @@
+// The block in the clear: arguments of the recurrence and norm kernels
+// (clear_scan.hip, clear_norm.hip), filled in and checked by clear.cpp.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fesc.h"
+
+namespace fesc {
+
+constexpr uint32_t kChunk = 64;   // tokens whose decay matrix is formed at once
+constexpr uint32_t kPTile = 64;   // channels of one head held by one workgroup
+constexpr uint32_t kMaxState = 128;
+
+// One direction of the recurrence over the sequence.  Forward: u = x, v = B,
+// states move from the first chunk to the last.  Reverse (the adjoint of the
+// states): u = dy, v = C, from the last chunk to the first.
+struct ScanDir {
+  const void* u;
+  const void* v;
+  int64_t u_token, u_batch, v_token, v_batch;
+  const float* init;   // [b][h][P][N] or null (zero)
+  float* fin;          // [b][h][P][N] or null
+  void* chunk_states;  // [b][h][chunk][P][N], element type of the call: the state that
+                       // enters each chunk; or null
+  float* seg_states;   // [b][h][segment][P][N] or null (one segment)
+  float* seg_decay;    // [b][h][segment]
+  bool reverse;
+};
+
+struct ScanShape {
+  uint32_t batch, len, heads, head_dim, groups, d_state;
+  uint32_t chunks;      // ceil(len / kChunk)
+  uint32_t seg_chunks;  // chunks per segment
+  uint32_t segs;
+  uint32_t ptiles;      // ceil(head_dim / kPTile)
+  const void* la;
+  int64_t la_token, la_batch;
+  bool vec;  // rows of x, B, C (dy) can be read 16 bytes at a time
+  bool st4;  // four neighbouring state entries lie in one aligned 16 bytes
+  bool ch4;  // four neighbouring channels of y / dx lie in one aligned word group
+};
+
+struct ScanOut {  // outputs of a forward scan beside the final state
+  const void* c;
+  int64_t c_token, c_batch;
+  void* y;
+};
+
+struct ScanGrad {
+  const void *x, *b, *c, *dy;
+  int64_t x_token, x_batch, b_token, b_batch, c_token, c_batch, dy_token, dy_batch;
+  const void *s_in, *r_in;  // chunk states of the two directions
+  void *dx, *dla, *db, *dc;
+  float *db_part, *dc_part;  // [split][b][t][G][N] when heads are split, else null
+  uint32_t splits, heads_per_split;
+};
+
+struct StepArgs {
+  const void *x, *la, *b, *c;
+  int64_t x_row, la_row, b_row, c_row;
+  float* state;
+  const int32_t* slots;
+  void* y;
+  uint32_t rows, pool, heads, head_dim, groups, d_state;
+  bool st4;
+};
+
+struct NormArgs {
+  uint64_t rows;
+  uint32_t width;
+  float eps;
+  const void *a, *b, *c;   // gated: m, x, z; residual: o, r
+  int64_t a_row, b_row, c_row;
+  const void *k, *w;       // skip or scale; weight
+  void *u, *r_new;
+  // backward
+  const void *du, *dr_new;
+  int64_t du_row, dr_row;
+  void *da, *db, *dc, *dk, *dw;
+  float* part;             // [blocks][2][width]
+  uint32_t blocks;
+  bool vec;
+};
+
+// Every state pass of a call: the segments' own states and their join (only
+// when there are several), then the chunk states and final states.
+hipError_t launch_scan_states(uint32_t dtype, const ScanShape& sh, const ScanDir* dirs, int ndirs,
+                              hipStream_t s);
+hipError_t launch_scan_out(uint32_t dtype, const ScanShape& sh, const ScanDir& dir,
+                           const ScanOut& out, hipStream_t s);
+hipError_t launch_scan_grad(uint32_t dtype, const ScanShape& sh, const ScanGrad& g, hipStream_t s);
+hipError_t launch_scan_step(uint32_t dtype, const StepArgs& a, hipStream_t s);
+hipError_t launch_state_copy(const float* from, float* to, uint64_t count, hipStream_t s);
+
+hipError_t launch_norm(uint32_t dtype, bool gated, const NormArgs& a, hipStream_t s);
+hipError_t launch_norm_grad(uint32_t dtype, bool gated, const NormArgs& a, hipStream_t s);
+uint32_t norm_grad_blocks(uint64_t rows, uint32_t width);
+
+}  // namespace fesc

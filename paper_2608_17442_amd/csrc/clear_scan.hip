@@ -1,0 +1,990 @@
+// The gated linear recurrence in the clear and its gradient.
+//
+//   S_t = e^{la_t} S_{t-1} + x_t B_t^T,   y_t = S_t C_t        (per head, S in R^{P x N})
+//
+// is computed in chunks of kChunk tokens.  With cum_s the sum of la from the
+// chunk's start up to and including s, and S the state that enters the chunk,
+//
+//   y_s = sum_{r <= s} e^{cum_s - cum_r} (C_s . B_r) x_r + e^{cum_s} S C_s
+//   S'  = e^{cum_Q} S + sum_r e^{cum_Q - cum_r} x_r B_r^T
+//
+// so the work is matrix products over 64 x 64 x N tiles (MFMA), and the state
+// stays in registers, in fp32, from chunk to chunk.  Products with the state
+// and with the matrix of decays take these operands rounded to the call's
+// type (one rounding on each path to an output, as large as that of the
+// output itself); the state's own update does not round: the weighted inputs
+// enter as three bf16 parts that sum to the fp32 value exactly.
+#include "clear.hpp"
+#include "fesc_internal.hpp"
+
+namespace fesc {
+
+namespace {
+
+constexpr int Q = kChunk;
+constexpr int PT = kPTile;
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// A matrix operand as the 16x16 tiles take it: lane l holds row (or column)
+// l % 16 and 8 of the 32 values along the axis that is summed over, which 8
+// being the same for both operands of a product.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<__bf16> {
+  using Frag = bf16x8;
+  using Four = bf16x4;
+  static constexpr int kUnit = 8;  // elements in 16 bytes
+  // Row padding of LDS tiles.  A row pitch of 8 words past a multiple of 32
+  // words puts the 8 rows of a 16-byte access, and the 4 rows of a
+  // transposing access, on distinct banks.
+  static constexpr int kPad = 16;
+};
+template <>
+struct Elem<float> {
+  using Frag = f32x8;
+  using Four = f32x4;
+  static constexpr int kUnit = 4;
+  static constexpr int kPad = 4;
+};
+
+__device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(const f32x8& a, const f32x8& b, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
+// Eight values that lie next to each other in an LDS row.
+__device__ __forceinline__ bf16x8 row_frag(const __bf16* p) {
+  return *reinterpret_cast<const bf16x8*>(p);
+}
+__device__ __forceinline__ f32x8 row_frag(const float* p) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p);
+  const f32x4 b = *reinterpret_cast<const f32x4*>(p + 4);
+  return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// Four values of one column of an LDS tile: rows row0 .. row0 + 3 at column
+// col0 + l % 16, row0 the same for the 16 lanes of a group.
+__device__ __forceinline__ bf16x4 col_four(const __bf16* tile, int pitch, int row0, int col0) {
+  const int i = threadIdx.x & 15;
+  const __bf16* p = tile + (row0 + (i >> 2)) * pitch + col0 + 4 * (i & 3);
+  const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) s16x4*)(p));
+  return __builtin_bit_cast(bf16x4, v);
+}
+__device__ __forceinline__ f32x4 col_four(const float* tile, int pitch, int row0, int col0) {
+  const float* p = tile + row0 * pitch + col0 + (threadIdx.x & 15);
+  return f32x4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
+}
+
+__device__ __forceinline__ bf16x8 join(const bf16x4& a, const bf16x4& b) {
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ f32x8 join(const f32x4& a, const f32x4& b) {
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+template <typename T>
+__device__ __forceinline__ typename Elem<T>::Four to_four(const f32x4& v) {
+  if constexpr (sizeof(T) == 4)
+    return v;
+  else
+    return __builtin_convertvector(v, bf16x4);
+}
+__device__ __forceinline__ f32x4 widen(const bf16x4& v) { return __builtin_convertvector(v, f32x4); }
+__device__ __forceinline__ f32x4 widen(const f32x4& v) { return v; }
+
+// The parts of a fp32 operand in the call's type: itself, or three bf16
+// values (each the leading 8 bits of what the ones before leave) whose sum it
+// is.
+template <typename T>
+struct Parts;
+template <>
+struct Parts<float> {
+  static constexpr int kCount = 1;
+  f32x8 p[1];
+  __device__ __forceinline__ Parts(const f32x4& a, const f32x4& b) { p[0] = join(a, b); }
+};
+template <>
+struct Parts<__bf16> {
+  static constexpr int kCount = 3;
+  bf16x8 p[3];
+  __device__ __forceinline__ Parts(const f32x4& a, const f32x4& b) {
+    f32x8 v = join(a, b);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        w[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]),
+                                     0x07060302u);
+      p[k] = __builtin_bit_cast(bf16x8, w);
+      if (k < 2) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+          v[j] = v[j] - hi;
+        }
+      }
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ float load1(const T* p) {
+  return (float)*p;
+}
+
+// Registers of one thread for a tile of ROWS x COLS elements on its way from
+// global memory to LDS; rows and columns past the valid ones are zero.
+template <typename T, int ROWS, int COLS, int THREADS>
+struct Stage {
+  static constexpr int kUnit = Elem<T>::kUnit;
+  static constexpr int kPerRow = COLS / kUnit;
+  static constexpr int kUnits = ROWS * kPerRow / THREADS;
+  static_assert(ROWS * kPerRow % THREADS == 0, "whole units per thread");
+  u32x4 r[kUnits];
+
+  __device__ __forceinline__ void load(const T* base, int64_t pitch, int rows, int cols,
+                                       bool vec) {
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      const int row = i / kPerRow, col = i % kPerRow * kUnit;
+      const T* p = base + row * pitch + col;
+      u32x4 v = {0, 0, 0, 0};
+      if (vec) {
+        if (row < rows && col < cols) v = *reinterpret_cast<const u32x4*>(p);
+      } else if (row < rows) {
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j) {
+          if (col + j < cols) {
+            if constexpr (sizeof(T) == 4)
+              v[j] = *reinterpret_cast<const uint32_t*>(p + j);
+            else
+              v[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + j) << (16 * (j & 1));
+          }
+        }
+      }
+      r[k] = v;
+    }
+  }
+  __device__ __forceinline__ void store(T* tile, int pitch) const {
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      *reinterpret_cast<u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit) = r[k];
+    }
+  }
+  // sum of the products of these values with those at the same places of a tile
+  __device__ __forceinline__ float dot(const T* tile, int pitch) const {
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      const u32x4 o =
+          *reinterpret_cast<const u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) {
+          s = __builtin_fmaf(__uint_as_float(r[k][j]), __uint_as_float(o[j]), s);
+        } else {
+          s = __builtin_fmaf(__uint_as_float(r[k][j] << 16), __uint_as_float(o[j] << 16), s);
+          s = __builtin_fmaf(__uint_as_float(r[k][j] & 0xffff0000u),
+                             __uint_as_float(o[j] & 0xffff0000u), s);
+        }
+      }
+    }
+    return s;
+  }
+};
+
+// Four neighbouring fp32 (state entries) with those at or past `left` absent.
+__device__ __forceinline__ f32x4 load_four(const float* p, int left, bool whole) {
+  if (whole) return left > 0 ? *reinterpret_cast<const f32x4*>(p) : f32x4{0, 0, 0, 0};
+  f32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = i < left ? p[i] : 0.0f;
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_four(T* p, const f32x4& v, int left, bool whole) {
+  if (whole) {
+    if (left > 0) *reinterpret_cast<typename Elem<T>::Four*>(p) = to_four<T>(v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) p[i] = (T)v[i];
+  }
+}
+
+// Running sums of the log decays (base 2) of a chunk, lane l the token l, in
+// fp64 and then as a pair of floats: hi a multiple of 2^-6, so that hi_s - hi_r
+// is exact and a difference of two sums is as accurate as a sum over the
+// tokens between them, whatever lies before them.  la below kReset (in
+// particular -inf: a reset) counts as kReset, whose decay is 0 in fp32.
+constexpr float kReset = -1000.0f;
+struct Cum {
+  float hi, lo;   // of token l
+  float e, w;     // e^{cum_l}, e^{cum_Q - cum_l}
+  float total;    // e^{cum_Q}
+};
+__device__ __forceinline__ float exp2_diff(float hs, float ls, float hr, float lr) {
+  return __builtin_amdgcn_exp2f((hs - hr) + (ls - lr));
+}
+__device__ __forceinline__ Cum cumulate(float la) {
+  constexpr double kLog2e = 1.4426950408889634;
+  double c = (double)(la < kReset ? kReset : la) * kLog2e;
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const double o = __shfl_up(c, d);
+    c += l >= d ? o : 0.0;
+  }
+  Cum r;
+  r.hi = (float)(__builtin_rint(c * 64.0) * (1.0 / 64.0));
+  r.lo = (float)(c - (double)r.hi);
+  const float th = __shfl(r.hi, 63), tl = __shfl(r.lo, 63);
+  r.e = exp2_diff(r.hi, r.lo, 0.0f, 0.0f);
+  r.w = exp2_diff(th, tl, r.hi, r.lo);
+  r.total = __builtin_amdgcn_exp2f(th + tl);
+  return r;
+}
+
+// ------------------------------------------------------------ scan kernels
+
+// One workgroup: one head's channel tile over the chunks of one segment.
+// Wave w holds the state rows p = 16 w + l % 16, entries n = 16 t + 4 g + i
+// (g = l / 16), i.e. the transpose of the state as MFMA result tiles.
+template <typename T, int NT>
+struct ScanTiles {
+  static constexpr int XS = PT + Elem<T>::kPad;
+  static constexpr int NS = NT + Elem<T>::kPad;
+};
+
+struct Where {
+  uint32_t b, h, pt, seg, g;
+};
+// Heads that read the same B and C rows lie `batch * segs` workgroups apart:
+// on one XCD where that is a multiple of 8.
+__device__ __forceinline__ Where where(const ScanShape& sh) {
+  Where w;
+  const uint32_t per = sh.batch * sh.segs, id = blockIdx.x;
+  const uint32_t bs = id % per, hp = id / per;
+  w.b = bs / sh.segs;
+  w.seg = bs % sh.segs;
+  w.h = hp / sh.ptiles;
+  w.pt = hp % sh.ptiles;
+  w.g = w.h / (sh.heads / sh.groups);
+  return w;
+}
+
+template <int NTILES>
+__device__ __forceinline__ void load_state(f32x4 (&s)[NTILES], const float* base, int p, int rows,
+                                           int N, bool st4) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int t = 0; t < NTILES; ++t) {
+    const int n = 16 * t + 4 * g;
+    s[t] = p < rows ? load_four(base + (int64_t)p * N + n, N - n, st4) : f32x4{0, 0, 0, 0};
+  }
+}
+template <int NTILES, typename T>
+__device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], T* base, int p, int rows,
+                                            int N, bool st4) {
+  const int g = (threadIdx.x & 63) >> 4;
+  if (p >= rows) return;
+#pragma unroll
+  for (int t = 0; t < NTILES; ++t) {
+    const int n = 16 * t + 4 * g;
+    store_four<T>(base + (int64_t)p * N + n, s[t], N - n, st4);
+  }
+}
+
+// S' = total S + sum_r w_r x_r B_r^T over the chunk in LDS.
+template <typename T, int NT>
+__device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16], const T* xs, const T* bs,
+                                             const float* w, float total, int wave) {
+  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int t = 0; t < NT / 16; ++t) s[t] *= total;
+#pragma unroll
+  for (int k0 = 0; k0 < Q; k0 += 32) {
+    const int r0 = k0 + 8 * g;
+    const f32x4 wa = *reinterpret_cast<const f32x4*>(w + r0);
+    const f32x4 wb = *reinterpret_cast<const f32x4*>(w + r0 + 4);
+    const Parts<T> x(widen(col_four(xs, XS, r0, 16 * wave)) * wa,
+                     widen(col_four(xs, XS, r0 + 4, 16 * wave)) * wb);
+#pragma unroll
+    for (int t = 0; t < NT / 16; ++t) {
+      const typename Elem<T>::Frag b =
+          join(col_four(bs, NS, r0, 16 * t), col_four(bs, NS, r0 + 4, 16 * t));
+#pragma unroll
+      for (int k = 0; k < Parts<T>::kCount; ++k) s[t] = mma(b, x.p[k], s[t]);
+    }
+  }
+}
+
+// States only.  Segment pass (`summaries`): each segment's own state, from
+// zero, and its total decay, to seg_states and seg_decay.  Otherwise from the
+// state that enters the segment: the states that enter the chunks, and the
+// final state.  Memory bound: u and v are read once, 4 P N bytes written per
+// segment or one state per chunk.
+template <typename T, int NT>
+__global__ __launch_bounds__(256) void k_scan_states(ScanShape sh, ScanDir d0, ScanDir d1,
+                                                     bool summaries) {
+  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+  __shared__ __align__(16) T xs[Q * XS];
+  __shared__ __align__(16) T bs[Q * NS];
+  __shared__ __align__(16) float wt[Q];
+  __shared__ float total;
+  const ScanDir& d = blockIdx.z ? d1 : d0;
+  const Where at = where(sh);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int P = sh.head_dim, N = sh.d_state;
+  const int p0 = at.pt * PT, rows = min(PT, P - p0), p = 16 * wave + (lane & 15);
+  // segments and chunks are counted in the direction of the pass
+  const int first = at.seg * sh.seg_chunks;
+  const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
+  if (summaries && at.seg + 1 == sh.segs) return;  // no segment follows the last
+  const uint64_t head = (uint64_t)at.b * sh.heads + at.h;
+  const uint64_t size = (uint64_t)P * N;
+  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + p0;
+  const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
+
+  f32x4 s[NT / 16];
+  const float* from = summaries       ? nullptr
+                      : d.seg_states ? d.seg_states + (head * sh.segs + at.seg) * size
+                      : d.init       ? d.init + head * size
+                                     : nullptr;
+  if (from) {
+    load_state(s, from + (uint64_t)p0 * N, p, rows, N, sh.st4);
+  } else {
+#pragma unroll
+    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
+  }
+  Stage<T, Q, PT, 256> xst;
+  Stage<T, Q, NT, 256> bst;
+  float lav = 0.0f;
+  auto fetch = [&](int k) {
+    const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
+    const int64_t t0 = (int64_t)c * Q;
+    const int n = min((int64_t)Q, (int64_t)sh.len - t0);
+    xst.load(u + t0 * d.u_token, d.u_token, n, rows, sh.vec);
+    bst.load(v + t0 * d.v_token, d.v_token, n, N, sh.vec);
+    lav = lane < n ? load1(la + (t0 + lane) * sh.la_token) : 0.0f;
+  };
+  fetch(0);
+  float decay = 1.0f;
+  for (int k = 0; k < count; ++k) {
+    if (d.chunk_states && !summaries) {
+      const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
+      store_state(s, (T*)d.chunk_states + (head * sh.chunks + c) * size + (uint64_t)p0 * N, p,
+                  rows, N, sh.st4);
+    }
+    Cum cum;
+    if (wave == 0) cum = cumulate(lav);
+    __syncthreads();
+    xst.store(xs, XS);
+    bst.store(bs, NS);
+    if (wave == 0) {
+      wt[lane] = d.reverse ? cum.e : cum.w;
+      if (lane == 0) total = cum.total;
+    }
+    __syncthreads();
+    if (k + 1 < count) fetch(k + 1);
+    update_state<T, NT>(s, xs, bs, wt, total, wave);
+    decay *= total;
+  }
+  if (summaries) {
+    store_state(s, d.seg_states + (head * sh.segs + at.seg + 1) * size + (uint64_t)p0 * N, p, rows,
+                N, sh.st4);
+    if (threadIdx.x == 0 && at.pt == 0) d.seg_decay[head * sh.segs + at.seg] = decay;
+  } else if (d.fin && at.seg + 1 == sh.segs) {
+    store_state(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N, sh.st4);
+  }
+}
+
+// Segment summaries to the states that enter the segments, in place: the
+// summary of segment j lies in the place of segment j + 1.
+__global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, ScanDir d1) {
+  const ScanDir& d = blockIdx.z ? d1 : d0;
+  const uint32_t size = sh.head_dim * sh.d_state, blocks = (size + 255) / 256;
+  const uint32_t e = blockIdx.x % blocks * 256 + threadIdx.x;
+  const uint64_t head = blockIdx.x / blocks;
+  if (e >= size) return;
+  float* s = d.seg_states + head * sh.segs * (uint64_t)size + e;
+  const float* decay = d.seg_decay + head * sh.segs;
+  float carry = d.init ? d.init[head * size + e] : 0.0f;
+  s[0] = carry;
+  for (uint32_t j = 1; j < sh.segs; ++j) {
+    float* at = s + (uint64_t)j * size;
+    carry = __builtin_fmaf(decay[j - 1], carry, *at);
+    *at = carry;
+  }
+}
+
+// Outputs and final state.
+template <typename T, int NT>
+__global__ __launch_bounds__(256) void k_scan_out(ScanShape sh, ScanDir d, ScanOut o) {
+  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+  __shared__ __align__(16) T xs[Q * XS];
+  __shared__ __align__(16) T bs[Q * NS];
+  __shared__ __align__(16) T cs[Q * NS];
+  __shared__ __align__(16) T ss[PT * NS];
+  __shared__ __align__(16) float hi[Q], lo[Q], ec[Q], wt[Q];
+  __shared__ float total;
+  using Frag = typename Elem<T>::Frag;
+  using Four = typename Elem<T>::Four;
+  const Where at = where(sh);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const int P = sh.head_dim, N = sh.d_state;
+  const int p0 = at.pt * PT, rows = min(PT, P - p0), p = 16 * wave + col;
+  const int first = at.seg * sh.seg_chunks;
+  const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
+  const uint64_t head = (uint64_t)at.b * sh.heads + at.h;
+  const uint64_t size = (uint64_t)P * N;
+  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + p0;
+  const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
+  const T* cc = (const T*)o.c + at.b * o.c_batch + (int64_t)at.g * N;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
+  T* y = (T*)o.y + ((uint64_t)at.b * sh.len * sh.heads + at.h) * P + p0;
+
+  f32x4 s[NT / 16];
+  const float* from = d.seg_states ? d.seg_states + (head * sh.segs + at.seg) * size
+                      : d.init     ? d.init + head * size
+                                   : nullptr;
+  if (from) {
+    load_state(s, from + (uint64_t)p0 * N, p, rows, N, sh.st4);
+  } else {
+#pragma unroll
+    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
+  }
+  Stage<T, Q, PT, 256> xst;
+  Stage<T, Q, NT, 256> bst, cst;
+  float lav = 0.0f;
+  auto fetch = [&](int k) {
+    const int64_t t0 = (int64_t)(first + k) * Q;
+    const int n = min((int64_t)Q, (int64_t)sh.len - t0);
+    xst.load(u + t0 * d.u_token, d.u_token, n, rows, sh.vec);
+    bst.load(v + t0 * d.v_token, d.v_token, n, N, sh.vec);
+    cst.load(cc + t0 * o.c_token, o.c_token, n, N, sh.vec);
+    lav = lane < n ? load1(la + (t0 + lane) * sh.la_token) : 0.0f;
+  };
+  fetch(0);
+  for (int k = 0; k < count; ++k) {
+    Cum cum;
+    if (wave == 0) cum = cumulate(lav);
+    __syncthreads();
+    xst.store(xs, XS);
+    bst.store(bs, NS);
+    cst.store(cs, NS);
+#pragma unroll
+    for (int t = 0; t < NT / 16; ++t)
+      *reinterpret_cast<Four*>(ss + p * NS + 16 * t + 4 * g) = to_four<T>(s[t]);
+    if (wave == 0) {
+      hi[lane] = cum.hi;
+      lo[lane] = cum.lo;
+      ec[lane] = cum.e;
+      wt[lane] = cum.w;
+      if (lane == 0) total = cum.total;
+    }
+    __syncthreads();
+    if (k + 1 < count) fetch(k + 1);
+
+    // Tokens s = 16 wave + col.  Tiles of (C B^T)^T have rows r and columns s:
+    // a lane's four values are the operand of the product with x that sums
+    // over r, so they never leave the registers.
+    Frag cf[NT / 32];
+#pragma unroll
+    for (int q = 0; q < NT / 32; ++q) cf[q] = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
+    const float hs = hi[16 * wave + col], ls = lo[16 * wave + col];
+    Four w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x4 acc = {0, 0, 0, 0};
+      if (j <= wave) {
+#pragma unroll
+        for (int q = 0; q < NT / 32; ++q)
+          acc = mma(row_frag(bs + (16 * j + col) * NS + 32 * q + 8 * g), cf[q], acc);
+        const f32x4 hr = *reinterpret_cast<const f32x4*>(hi + 16 * j + 4 * g);
+        const f32x4 lr = *reinterpret_cast<const f32x4*>(lo + 16 * j + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool seen = j < wave || 4 * g + i <= col;
+          acc[i] = seen ? acc[i] * exp2_diff(hs, ls, hr[i], lr[i]) : 0.0f;
+        }
+      }
+      w[j] = to_four<T>(acc);
+    }
+    // y^T: rows p = 16 t + 4 g + i, column s
+    const float es = ec[16 * wave + col];
+    const int64_t ts = (int64_t)(first + k) * Q + 16 * wave + col;
+#pragma unroll
+    for (int t = 0; t < PT / 16; ++t) {
+      f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+      for (int q = 0; q < NT / 32; ++q)
+        acc = mma(row_frag(ss + (16 * t + col) * NS + 32 * q + 8 * g), cf[q], acc);
+      acc *= es;
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        if (j <= wave) {
+          const Frag xf = join(col_four(xs, XS, 16 * j + 4 * g, 16 * t),
+                               col_four(xs, XS, 16 * j + 16 + 4 * g, 16 * t));
+          acc = mma(xf, join(w[j], w[j + 1]), acc);
+        }
+      }
+      const int pp = 16 * t + 4 * g;
+      if (ts < (int64_t)sh.len)
+        store_four<T>(y + ts * sh.heads * P + pp, acc, rows - pp, sh.ch4);
+    }
+    update_state<T, NT>(s, xs, bs, wt, total, wave);
+  }
+  if (d.fin && at.seg + 1 == sh.segs)
+    store_state(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N, sh.st4);
+}
+
+// ------------------------------------------------------------ gradient
+
+// Gradients of one chunk, all heads of a split in turn (their sum is dB and
+// dC).  S the state that enters the chunk, R the adjoint of the one that
+// leaves it, K_{s,r} = dy_s . x_r, G_{s,r} = C_s . B_r, D_{s,r} = e^{cum_s - cum_r}
+// (0 for r > s), w_r = e^{cum_Q - cum_r}:
+//   dx_r = sum_s (D G)_{s,r} dy_s + w_r R B_r
+//   dC_s = sum_r W_{s,r} B_r + sum_h e^{cum_s} S^T dy_s,   W = sum_h D K
+//   dB_r = sum_s W_{s,r} C_s + sum_h w_r R^T x_r
+//   dla_t = sum_{s >= t > r} (D K G)_{s,r} + sum_{s >= t} C_s . (e^{cum_s} S^T dy_s)
+//           + sum_{r < t} B_r . (w_r R^T x_r) + e^{cum_Q} <R, S>
+// The first sum of dla falls from t to t + 1 by row sum minus column sum of
+// D K G at t.  Waves 0..3 hold the 16 columns r of G, K and W and form dx;
+// waves 4..7 hold 16 tokens of dC and dB.
+template <typename T, int NT>
+__global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
+  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+  __shared__ __align__(16) T bs[Q * NS];
+  __shared__ __align__(16) T cs[Q * NS];
+  __shared__ __align__(16) T xs[Q * XS];
+  __shared__ __align__(16) T dys[Q * XS];
+  __shared__ __align__(16) T sr[PT * NS];
+  __shared__ __align__(16) float hi[Q], lo[Q], ec[Q], wt[Q];
+  __shared__ float us[Q], vs[Q], colsum[Q], rowsum[4][Q], dots[8];
+  using Frag = typename Elem<T>::Frag;
+  using Four = typename Elem<T>::Four;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const bool left = wave < 4;  // waves of dx
+  const int tile = wave & 3;
+  const int P = sh.head_dim, N = sh.d_state;
+  const uint32_t bc = blockIdx.x;
+  const uint32_t b = bc / sh.chunks, c = bc % sh.chunks;
+  const uint32_t grp = blockIdx.y / a.splits, split = blockIdx.y % a.splits;
+  const int64_t t0 = (int64_t)c * Q;
+  const int n = min((int64_t)Q, (int64_t)sh.len - t0);
+  const uint32_t per_group = sh.heads / sh.groups;
+  const uint32_t h0 = split * a.heads_per_split;
+  const uint32_t hn = min(a.heads_per_split, per_group - h0);
+  const uint64_t size = (uint64_t)P * N;
+
+  {
+    Stage<T, Q, NT, 512> st;
+    st.load((const T*)a.b + b * a.b_batch + t0 * a.b_token + (int64_t)grp * N, a.b_token, n, N,
+            sh.vec);
+    st.store(bs, NS);
+    st.load((const T*)a.c + b * a.c_batch + t0 * a.c_token + (int64_t)grp * N, a.c_token, n, N,
+            sh.vec);
+    st.store(cs, NS);
+  }
+  Stage<T, Q, PT, 512> xst, dyst;
+  Stage<T, PT, NT, 512> sst, rst;
+  float lav = 0.0f;
+  auto fetch = [&](uint32_t k) {  // k: head of the split and channel tile
+    const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
+    const int p0 = pt * PT, rows = min(PT, P - p0);
+    xst.load((const T*)a.x + b * a.x_batch + t0 * a.x_token + (int64_t)h * P + p0, a.x_token, n,
+             rows, sh.vec);
+    dyst.load((const T*)a.dy + b * a.dy_batch + t0 * a.dy_token + (int64_t)h * P + p0, a.dy_token,
+              n, rows, sh.vec);
+    const uint64_t at = (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size + (uint64_t)p0 * N;
+    sst.load((const T*)a.s_in + at, N, rows, N, sh.vec);
+    rst.load((const T*)a.r_in + at, N, rows, N, sh.vec);
+    lav = lane < n ? load1((const T*)sh.la + b * sh.la_batch + (t0 + lane) * sh.la_token + h)
+                   : 0.0f;
+  };
+  fetch(0);
+  __syncthreads();
+
+  // waves 0..3: tiles (s = 16 j + 4 g + i, r = 16 tile + col) of G and W;
+  // waves 4..7: (n = 16 t + 4 g + i, token 16 tile + col) of dC and dB
+  f32x4 gt[4], wk[4];
+  f32x4 dc[NT / 16], db[NT / 16];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) gt[j] = wk[j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int t = 0; t < NT / 16; ++t) dc[t] = db[t] = f32x4{0, 0, 0, 0};
+  if (left) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j >= tile) {
+#pragma unroll
+        for (int q = 0; q < NT; q += 32)
+          gt[j] = mma(row_frag(cs + (16 * j + col) * NS + q + 8 * g),
+                      row_frag(bs + (16 * tile + col) * NS + q + 8 * g), gt[j]);
+      }
+    }
+  }
+  float dla = 0.0f;  // wave 0: token `lane`, summed over the channel tiles of a head
+  const uint32_t rounds = hn * sh.ptiles;
+  for (uint32_t k = 0; k < rounds; ++k) {
+    const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
+    const int p0 = pt * PT, rows = min(PT, P - p0);
+    Cum cum;
+    if (wave == 0) cum = cumulate(lav);
+    const bool reset = lav < kReset;
+    __syncthreads();
+    xst.store(xs, XS);
+    dyst.store(dys, XS);
+    sst.store(sr, NS);
+    if (wave == 0) {
+      hi[lane] = cum.hi;
+      lo[lane] = cum.lo;
+      ec[lane] = cum.e;
+      wt[lane] = cum.w;
+    }
+    __syncthreads();
+    Four dg[4];  // D G as an operand, summed over s
+    if (left) {
+      const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
+      float cols = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f32x4 m = {0, 0, 0, 0}, e = {0, 0, 0, 0};
+        if (j >= tile) {
+#pragma unroll
+          for (int q = 0; q < PT; q += 32)
+            m = mma(row_frag(dys + (16 * j + col) * XS + q + 8 * g),
+                    row_frag(xs + (16 * tile + col) * XS + q + 8 * g), m);
+          const f32x4 hs = *reinterpret_cast<const f32x4*>(hi + 16 * j + 4 * g);
+          const f32x4 ls = *reinterpret_cast<const f32x4*>(lo + 16 * j + 4 * g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool seen = j > tile || 4 * g + i >= col;
+            e[i] = seen ? exp2_diff(hs[i], ls[i], hr, lr) : 0.0f;
+            m[i] = seen ? m[i] * e[i] : 0.0f;
+          }
+          wk[j] += m;
+          e *= gt[j];
+          m *= gt[j];
+        }
+        dg[j] = to_four<T>(e);
+        cols += (m[0] + m[1]) + (m[2] + m[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float s = m[i];
+#pragma unroll
+          for (int x = 1; x < 16; x *= 2) s += __shfl_xor(s, x);
+          if (col == 0) rowsum[tile][16 * j + 4 * g + i] = s;
+        }
+      }
+      cols += __shfl_xor(cols, 16);
+      cols += __shfl_xor(cols, 32);
+      if (g == 0) colsum[16 * tile + col] = cols;
+    } else {
+      const float es = ec[16 * tile + col];
+      float sum = 0.0f;
+#pragma unroll
+      for (int t = 0; t < NT / 16; ++t) {
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < PT; q += 32)
+          acc = mma(join(col_four(sr, NS, q + 8 * g, 16 * t), col_four(sr, NS, q + 8 * g + 4, 16 * t)),
+                    row_frag(dys + (16 * tile + col) * XS + q + 8 * g), acc);
+        acc *= es;
+        dc[t] += acc;
+        const f32x4 cv =
+            widen(*reinterpret_cast<const Four*>(cs + (16 * tile + col) * NS + 16 * t + 4 * g));
+        sum += (acc[0] * cv[0] + acc[1] * cv[1]) + (acc[2] * cv[2] + acc[3] * cv[3]);
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (g == 0) us[16 * tile + col] = sum;
+    }
+    float dot = rst.dot(sr, NS);
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) dot += __shfl_xor(dot, x);
+    if (lane == 0) dots[wave] = dot;
+    __syncthreads();
+    rst.store(sr, NS);
+    __syncthreads();
+    if (k + 1 < rounds) fetch(k + 1);
+    if (left) {
+      const float wr = wt[16 * tile + col];
+      Frag bf[NT / 32];
+#pragma unroll
+      for (int q = 0; q < NT / 32; ++q)
+        bf[q] = row_frag(bs + (16 * tile + col) * NS + 32 * q + 8 * g);
+      const int64_t t = t0 + 16 * tile + col;
+      T* dx = (T*)a.dx + (((uint64_t)b * sh.len + t) * sh.heads + h) * P + p0;
+#pragma unroll
+      for (int x = 0; x < PT / 16; ++x) {
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < NT / 32; ++q)
+          acc = mma(row_frag(sr + (16 * x + col) * NS + 32 * q + 8 * g), bf[q], acc);
+        acc *= wr;
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          if (j + 1 >= tile) {
+            const Frag df = join(col_four(dys, XS, 16 * j + 4 * g, 16 * x),
+                                 col_four(dys, XS, 16 * j + 16 + 4 * g, 16 * x));
+            acc = mma(df, join(dg[j], dg[j + 1]), acc);
+          }
+        }
+        const int pp = 16 * x + 4 * g;
+        if (t < (int64_t)sh.len) store_four<T>(dx + pp, acc, rows - pp, sh.ch4);
+      }
+    } else {
+      const float wr = wt[16 * tile + col];
+      float sum = 0.0f;
+#pragma unroll
+      for (int t = 0; t < NT / 16; ++t) {
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < PT; q += 32)
+          acc = mma(join(col_four(sr, NS, q + 8 * g, 16 * t), col_four(sr, NS, q + 8 * g + 4, 16 * t)),
+                    row_frag(xs + (16 * tile + col) * XS + q + 8 * g), acc);
+        acc *= wr;
+        db[t] += acc;
+        const f32x4 bv =
+            widen(*reinterpret_cast<const Four*>(bs + (16 * tile + col) * NS + 16 * t + 4 * g));
+        sum += (acc[0] * bv[0] + acc[1] * bv[1]) + (acc[2] * bv[2] + acc[3] * bv[3]);
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (g == 0) vs[16 * tile + col] = sum;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      float base = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) base += dots[x];
+      const float u = us[lane] +
+                      ((rowsum[0][lane] + rowsum[1][lane]) + (rowsum[2][lane] + rowsum[3][lane])) -
+                      colsum[lane];
+      const float v = vs[lane];
+      float after = u, before = v;  // sums from the token on, and up to it
+#pragma unroll
+      for (int x = 1; x < 64; x *= 2) {
+        const float p = __shfl_down(after, x), q = __shfl_up(before, x);
+        after += lane + x < 64 ? p : 0.0f;
+        before += lane >= x ? q : 0.0f;
+      }
+      const float upto = __shfl_up(before, 1);
+      // before a reset nothing counts: the exact zero, not the sums' remainder
+      dla += reset ? 0.0f : after + (lane ? upto : 0.0f) + base * cum.total;
+      if (pt + 1 == sh.ptiles) {
+        if (lane < n)
+          ((T*)a.dla)[((uint64_t)b * sh.len + t0 + lane) * sh.heads + h] = (T)dla;
+        dla = 0.0f;
+      }
+    }
+  }
+  // W to LDS (rows s, columns r), then its products with B and C
+  if (left) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xs[(16 * j + 4 * g + i) * XS + 16 * tile + col] = (T)wk[j][i];
+  }
+  __syncthreads();
+  if (left) return;
+  const int64_t t = t0 + 16 * tile + col;
+  const uint64_t row = (((uint64_t)b * sh.len + t) * sh.groups + grp) * N;
+  const uint64_t part = (uint64_t)split * sh.batch * sh.len * sh.groups * N + row;
+  Frag wc[2], wb[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    wc[q] = row_frag(xs + (16 * tile + col) * XS + 32 * q + 8 * g);
+    wb[q] = join(col_four(xs, XS, 32 * q + 8 * g, 16 * tile),
+                 col_four(xs, XS, 32 * q + 8 * g + 4, 16 * tile));
+  }
+#pragma unroll
+  for (int x = 0; x < NT / 16; ++x) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      dc[x] = mma(join(col_four(bs, NS, 32 * q + 8 * g, 16 * x),
+                       col_four(bs, NS, 32 * q + 8 * g + 4, 16 * x)), wc[q], dc[x]);
+      db[x] = mma(join(col_four(cs, NS, 32 * q + 8 * g, 16 * x),
+                       col_four(cs, NS, 32 * q + 8 * g + 4, 16 * x)), wb[q], db[x]);
+    }
+    const int nn = 16 * x + 4 * g;
+    if (t < (int64_t)sh.len) {
+      if (a.db_part) {
+        store_four<float>(a.dc_part + part + nn, dc[x], N - nn, sh.st4);
+        store_four<float>(a.db_part + part + nn, db[x], N - nn, sh.st4);
+      } else {
+        store_four<T>((T*)a.dc + row + nn, dc[x], N - nn, sh.st4);
+        store_four<T>((T*)a.db + row + nn, db[x], N - nn, sh.st4);
+      }
+    }
+  }
+}
+
+// Sum of the splits' parts of dB (blockIdx.y = 0) or dC (1), in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_scan_parts(ScanGrad a, uint64_t count) {
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= count) return;
+  const float* p = (blockIdx.y ? a.dc_part : a.db_part) + i;
+  float s = p[0];
+  for (uint32_t k = 1; k < a.splits; ++k) s += p[k * count];
+  ((T*)(blockIdx.y ? a.dc : a.db))[i] = (T)s;
+}
+
+// ------------------------------------------------------------ one token
+
+// One served token per row: S = e^{la} S + x B^T in place, y = S C.  Memory
+// bound by the state, which is read and written once.  LPR lanes share one
+// state row, four entries each.
+template <typename T, int LPR>
+__global__ __launch_bounds__(256) void k_scan_step(StepArgs a, uint32_t psplit) {
+  constexpr int kRows = 256 / LPR;  // state rows per pass of the workgroup
+  const uint32_t ps = blockIdx.x % psplit;
+  const uint64_t rh = blockIdx.x / psplit;
+  const uint32_t h = rh % a.heads;
+  const uint64_t row = rh / a.heads;
+  const int P = a.head_dim, N = a.d_state;
+  const int n = threadIdx.x % LPR * 4, sub = threadIdx.x / LPR;
+  const int64_t slot = a.slots ? (int64_t)a.slots[row] : (int64_t)row;
+  T* y = (T*)a.y + (row * a.heads + h) * P;
+  if (slot < 0 || slot >= (int64_t)a.pool) {  // an idle row
+    for (int p = ps * kRows + sub; p < P; p += psplit * kRows)
+      if (n == 0) y[p] = (T)0.0f;
+    return;
+  }
+  const uint32_t g = h / (a.heads / a.groups);
+  const T* x = (const T*)a.x + row * a.x_row + (int64_t)h * P;
+  const T* bp = (const T*)a.b + row * a.b_row + (int64_t)g * N + n;
+  const T* cp = (const T*)a.c + row * a.c_row + (int64_t)g * N + n;
+  const float decay = expf(load1((const T*)a.la + row * a.la_row + h));
+  f32x4 b, c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    b[i] = n + i < N ? load1(bp + i) : 0.0f;
+    c[i] = n + i < N ? load1(cp + i) : 0.0f;
+  }
+  float* s = a.state + ((uint64_t)slot * a.heads + h) * P * N + n;
+  for (int p = ps * kRows + sub; p < P; p += psplit * kRows) {
+    float* sp = s + (int64_t)p * N;
+    f32x4 v = load_four(sp, N - n, a.st4);
+    const float xv = load1(x + p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(decay, v[i], xv * b[i]);
+    store_four<float>(sp, v, N - n, a.st4);
+    float d = (v[0] * c[0] + v[1] * c[1]) + (v[2] * c[2] + v[3] * c[3]);
+#pragma unroll
+    for (int k = 1; k < LPR; k *= 2) d += __shfl_xor(d, k);
+    if (n == 0) y[p] = (T)d;
+  }
+}
+
+__global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to, uint64_t count) {
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < count) to[i] = from ? from[i] : 0.0f;
+}
+
+template <typename T, int NT>
+hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
+  const ScanDir &d0 = d[0], &d1 = d[nd - 1];
+  const dim3 grid(sh.batch * sh.segs * sh.heads * sh.ptiles, 1, nd);
+  if (sh.segs > 1) {
+    k_scan_states<T, NT><<<grid, 256, 0, s>>>(sh, d0, d1, true);
+    if (hipError_t e = hipGetLastError()) return e;
+    const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
+    k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  if (!main) return hipSuccess;
+  k_scan_states<T, NT><<<grid, 256, 0, s>>>(sh, d0, d1, false);
+  return hipGetLastError();
+}
+
+// One instance per element type and padded state size.
+#define FESC_SCAN_CASES(DTYPE, N, CALL)                      \
+  ((DTYPE) == FESC_BF16 ? ((N) <= 64 ? CALL(__bf16, 64) : CALL(__bf16, 128)) \
+                        : ((N) <= 64 ? CALL(float, 64) : CALL(float, 128)))
+
+}  // namespace
+
+hipError_t launch_scan_states(uint32_t dtype, const ScanShape& sh, const ScanDir* d, int nd,
+                              hipStream_t s) {
+#define CALL(T, NT) states<T, NT>(sh, d, nd, true, s)
+  return FESC_SCAN_CASES(dtype, sh.d_state, CALL);
+#undef CALL
+}
+
+hipError_t launch_scan_out(uint32_t dtype, const ScanShape& sh, const ScanDir& d,
+                           const ScanOut& o, hipStream_t s) {
+#define CALL(T, NT) states<T, NT>(sh, &d, 1, false, s)
+  if (hipError_t e = FESC_SCAN_CASES(dtype, sh.d_state, CALL)) return e;
+#undef CALL
+  const uint32_t grid = sh.batch * sh.segs * sh.heads * sh.ptiles;
+#define CALL(T, NT) (k_scan_out<T, NT><<<grid, 256, 0, s>>>(sh, d, o), hipGetLastError())
+  return FESC_SCAN_CASES(dtype, sh.d_state, CALL);
+#undef CALL
+}
+
+hipError_t launch_scan_grad(uint32_t dtype, const ScanShape& sh, const ScanGrad& g,
+                            hipStream_t s) {
+  const dim3 grid(sh.batch * sh.chunks, sh.groups * g.splits);
+#define CALL(T, NT) (k_scan_grad<T, NT><<<grid, 512, 0, s>>>(sh, g), hipGetLastError())
+  hipError_t e = FESC_SCAN_CASES(dtype, sh.d_state, CALL);
+#undef CALL
+  if (e || g.splits == 1) return e;
+  const uint64_t count = (uint64_t)sh.batch * sh.len * sh.groups * sh.d_state;
+  const dim3 pgrid((uint32_t)((count + 255) / 256), 2);
+  if (dtype == FESC_BF16)
+    k_scan_parts<__bf16><<<pgrid, 256, 0, s>>>(g, count);
+  else
+    k_scan_parts<float><<<pgrid, 256, 0, s>>>(g, count);
+  return hipGetLastError();
+}
+
+hipError_t launch_scan_step(uint32_t dtype, const StepArgs& a, hipStream_t s) {
+  const uint32_t lpr = a.d_state <= 64 ? 16 : 32, rows = 256 / lpr;
+  const uint32_t passes = (a.head_dim + rows - 1) / rows;
+  const uint64_t heads = (uint64_t)a.rows * a.heads;
+  // a few rows only: one pass per workgroup, so that all compute units work
+  const uint32_t psplit = heads >= 2048 ? 1 : passes;
+  const uint32_t grid = (uint32_t)(heads * psplit);
+#define STEP(T)                                                       \
+  if (lpr == 16)                                                      \
+    k_scan_step<T, 16><<<grid, 256, 0, s>>>(a, psplit);               \
+  else                                                                \
+    k_scan_step<T, 32><<<grid, 256, 0, s>>>(a, psplit)
+  if (dtype == FESC_BF16) {
+    STEP(__bf16);
+  } else {
+    STEP(float);
+  }
+#undef STEP
+  return hipGetLastError();
+}
+
+hipError_t launch_state_copy(const float* from, float* to, uint64_t count, hipStream_t s) {
+  k_state_copy<<<dim3((uint32_t)((count + 255) / 256)), 256, 0, s>>>(from, to, count);
+  return hipGetLastError();
+}
+
+}  // namespace fesc

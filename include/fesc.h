@@ -778,7 +778,8 @@ int fesc_calib_hbm(fesc_ctx* ctx, int kind, size_t bytes, double* rate, void* st
  * B and C [batch][len][groups][d_state]; dy like x.  y, dx, dla, db and dc
  * are contiguous; states are contiguous float [batch][heads][head_dim][d_state].
  * 1 <= d_state <= 128, 1 <= head_dim <= 4096, heads <= 4096 and a multiple of
- * groups.  batch or len may be 0. */
+ * groups, heads * head_dim and every token stride at most 2^22.  batch or len
+ * may be 0. */
 typedef struct fesc_clear_scan_desc {
   uint32_t dtype;
   uint32_t batch, len;

@@ -16,7 +16,6 @@ from __future__ import annotations
 import ctypes
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from .fesc import _check, _lib
 
@@ -59,8 +58,14 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream():
-    return torch.cuda.current_stream().cuda_stream
+def _stream(t):
+    """The current stream of t's device, as its handle."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _once():
+    if torch.is_grad_enabled():
+        raise RuntimeError("the block in the clear is differentiable once: no create_graph=True")
 
 
 def _tensor(t, what, like=None, dtype=None):
@@ -139,7 +144,7 @@ def _scan_forward(x, la, B, C, h0, want_state):
     need = _space(d, _lib.fesc_clear_scan_workspace, 0)
     w = _buffer(need, x)
     _check(_lib.fesc_clear_scan(ctypes.byref(d), _p(x), _p(la), _p(B), _p(C), _p(h0), _p(y),
-                                _p(h), _p(w), need, _stream()))
+                                _p(h), _p(w), need, _stream(x)))
     return y, h
 
 
@@ -152,8 +157,8 @@ class _Scan(torch.autograd.Function):
         return (y, h) if want_state else y
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, dy, dh=None):
+        _once()
         x, la, B, C, h0 = ctx.saved_tensors
         if dy is None:
             if dh is None:
@@ -175,7 +180,7 @@ class _Scan(torch.autograd.Function):
         w = _buffer(need, x)
         _check(_lib.fesc_clear_scan_bwd(
             ctypes.byref(d), _p(x), _p(la), _p(B), _p(C), _p(h0), _p(dy), _p(dh), _p(dx), _p(dla),
-            _p(db), _p(dc), _p(dh0), _p(w), need, _stream()))
+            _p(db), _p(dc), _p(dh0), _p(w), need, _stream(x)))
         return dx, dla, db, dc, dh0, None
 
 
@@ -246,7 +251,7 @@ def scan_step(x, la, B, C, state, slots=None, stream=None):
     d = _ScanDesc(_TYPES[x.dtype], rows, 1, H, P, G, N, 0, x.stride(0), 0, la.stride(0), 0,
                   B.stride(0), 0, C.stride(0), 0, 0)
     _check(_lib.fesc_clear_scan_step(ctypes.byref(d), _p(x), _p(la), _p(B), _p(C), _p(state),
-                                     state.shape[0], _p(slots), _p(y), _stream()))
+                                     state.shape[0], _p(slots), _p(y), _stream(x)))
     return y
 
 
@@ -309,7 +314,7 @@ def _gated_forward(m, x, z, skip, w, eps):
     d = _norm_desc(m, eps, m_row=_rows(m, "m"), x_row=_rows(x, "x"), z_row=_rows(z, "z"))
     u = _empty(m)
     _check(_lib.fesc_clear_norm_gated(ctypes.byref(d), _p(m), _p(x), _p(z), _p(skip), _p(w), _p(u),
-                                      _stream()))
+                                      _stream(m)))
     return u
 
 
@@ -321,8 +326,8 @@ class _Gated(torch.autograd.Function):
         return _gated_forward(m, x, z, skip, w, eps)
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, du):
+        _once()
         m, x, z, skip, w = ctx.saved_tensors
         du, du_row = _grad_rows(du)
         d = _norm_desc(m, ctx.eps, m_row=_rows(m, "m"), x_row=_rows(x, "x"), z_row=_rows(z, "z"),
@@ -332,7 +337,7 @@ class _Gated(torch.autograd.Function):
         ws = _buffer(need, m)
         _check(_lib.fesc_clear_norm_gated_bwd(
             ctypes.byref(d), _p(m), _p(x), _p(z), _p(skip), _p(w), _p(du), _p(dm), _p(dx), _p(dz),
-            _p(dskip), _p(dw), _p(ws), need, _stream()))
+            _p(dskip), _p(dw), _p(ws), need, _stream(m)))
         return dm, dx, dz, dskip, dw, None
 
 
@@ -355,7 +360,7 @@ def _residual_forward(o, r, scale, w, eps):
     d = _norm_desc(o, eps, o_row=_rows(o, "o"), r_row=_rows(r, "r"))
     new, u = _empty(o), _empty(o)
     _check(_lib.fesc_clear_norm_residual(ctypes.byref(d), _p(o), _p(r), _p(scale), _p(w), _p(new),
-                                         _p(u), _stream()))
+                                         _p(u), _stream(o)))
     return new, u
 
 
@@ -368,8 +373,8 @@ class _Residual(torch.autograd.Function):
         return _residual_forward(o, r, scale, w, eps)
 
     @staticmethod
-    @once_differentiable
     def backward(ctx, dnew, du):
+        _once()
         o, r, scale, w = ctx.saved_tensors
         if dnew is None and du is None:
             return (None,) * 5
@@ -383,7 +388,7 @@ class _Residual(torch.autograd.Function):
         ws = _buffer(need, o)
         _check(_lib.fesc_clear_norm_residual_bwd(
             ctypes.byref(d), _p(o), _p(r), _p(scale), _p(w), _p(du), _p(dnew), _p(do), _p(dr),
-            _p(dscale), _p(dw), _p(ws), need, _stream()))
+            _p(dscale), _p(dw), _p(ws), need, _stream(o)))
         return do, dr, dscale, dw, None
 
 

@@ -15,6 +15,8 @@ namespace {
 hipStream_t S(void* stream) { return reinterpret_cast<hipStream_t>(stream); }
 
 constexpr uint64_t kMaxStride = 1ull << 40;
+// A chunk's rows lie within 2^31 bytes of its first one.
+constexpr uint64_t kMaxTokenStride = 1ull << 22;
 // A launch counts its work items in 32 bits.
 constexpr uint64_t kMaxGrid256 = 1ull << 24, kMaxGrid512 = 1ull << 23;
 
@@ -30,9 +32,12 @@ int check_scan(const fesc_clear_scan_desc* d) {
     return fail(FESC_ERR_ARG, "heads: 1..4096 and a multiple of groups");
   if (d->head_dim == 0 || d->head_dim > 4096) return fail(FESC_ERR_ARG, "head_dim: 1..4096");
   if (d->d_state == 0 || d->d_state > kMaxState) return fail(FESC_ERR_ARG, "d_state: 1..128");
-  for (uint64_t s : {d->x_token, d->x_batch, d->la_token, d->la_batch, d->b_token, d->b_batch,
-                     d->c_token, d->c_batch, d->dy_token, d->dy_batch})
-    if (s > kMaxStride) return fail(FESC_ERR_ARG, "stride too large");
+  for (uint64_t s : {d->x_batch, d->la_batch, d->b_batch, d->c_batch, d->dy_batch})
+    if (s > kMaxStride) return fail(FESC_ERR_ARG, "batch strides: at most 2^40");
+  for (uint64_t s : {d->x_token, d->la_token, d->b_token, d->c_token, d->dy_token})
+    if (s > kMaxTokenStride) return fail(FESC_ERR_ARG, "token strides: at most 2^22");
+  if (d->heads * d->head_dim > kMaxTokenStride || d->groups * d->d_state > kMaxTokenStride)
+    return fail(FESC_ERR_ARG, "heads * head_dim: at most 2^22");
   return FESC_OK;
 }
 
@@ -41,7 +46,7 @@ struct Rows {
   uint32_t per;  // elements in 16 bytes
   bool ok = true;
   explicit Rows(uint32_t dtype) : per(16 / elem_bytes(dtype)) {}
-  Rows& add(const void* p, uint64_t s0, uint64_t s1 = 0) {
+  Rows& add(const void* p, uint64_t s0 = 0, uint64_t s1 = 0) {
     ok = ok && aligned(p, 16) && s0 % per == 0 && s1 % per == 0;
     return *this;
   }
@@ -141,10 +146,6 @@ int check_workspace(const void* p, size_t have, size_t need) {
   return FESC_OK;
 }
 
-bool word_groups(const ScanShape& s, uint32_t dtype, const void* p) {
-  return s.head_dim % 4 == 0 && aligned(p, 4 * elem_bytes(dtype));
-}
-
 int check_norm(const fesc_clear_norm_desc* d) {
   if (!d) return fail(FESC_ERR_ARG, "null descriptor");
   if (d->dtype != FESC_F32 && d->dtype != FESC_BF16)
@@ -230,9 +231,8 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
   if (int rc = check_workspace(workspace, workspace_bytes, w.used)) return rc;
   s.la = la;
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
-              .add(C, d->c_token, d->c_batch).len(d->head_dim).len(d->d_state).ok;
-  s.st4 = d->d_state % 4 == 0 && aligned(h0, 16) && aligned(hT, 16);
-  s.ch4 = word_groups(s, d->dtype, y);
+              .add(C, d->c_token, d->c_batch).add(h0).add(hT).add(y).len(d->head_dim)
+              .len(d->d_state).ok;
   dir.u = x;
   dir.v = B;
   dir.u_token = d->x_token;
@@ -265,11 +265,8 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
   if (int rc = check_workspace(workspace, workspace_bytes, w.used)) return rc;
   s.la = la;
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
-              .add(C, d->c_token, d->c_batch).add(dy, d->dy_token, d->dy_batch).len(d->head_dim)
-              .len(d->d_state).ok;
-  s.st4 = d->d_state % 4 == 0 && aligned(h0, 16) && aligned(dhT, 16) && aligned(dh0, 16) &&
-          aligned(db, 16) && aligned(dc, 16);
-  s.ch4 = word_groups(s, d->dtype, dx);
+              .add(C, d->c_token, d->c_batch).add(dy, d->dy_token, d->dy_batch).add(h0).add(dhT)
+              .add(dh0).add(dx).add(db).add(dc).len(d->head_dim).len(d->d_state).ok;
   dir[0].u = x;
   dir[0].v = B;
   dir[0].u_token = d->x_token;
@@ -336,7 +333,7 @@ int fesc_clear_scan_step(const fesc_clear_scan_desc* d, const void* x, const voi
   a.head_dim = d->head_dim;
   a.groups = d->groups;
   a.d_state = d->d_state;
-  a.st4 = d->d_state % 4 == 0 && aligned(state, 16);
+  a.vec = d->d_state % 4 == 0 && aligned(state, 16);
   return hip_check(launch_scan_step(d->dtype, a, S(stream)), "scan step");
 }
 

@@ -37,9 +37,7 @@ struct ScanShape {
   uint32_t ptiles;      // ceil(head_dim / kPTile)
   const void* la;
   int64_t la_token, la_batch;
-  bool vec;  // rows of x, B, C (dy) can be read 16 bytes at a time
-  bool st4;  // four neighbouring state entries lie in one aligned 16 bytes
-  bool ch4;  // four neighbouring channels of y / dx lie in one aligned word group
+  bool vec;  // every row of every array starts at a multiple of 16 bytes
 };
 
 struct ScanOut {  // outputs of a forward scan beside the final state
@@ -64,7 +62,7 @@ struct StepArgs {
   const int32_t* slots;
   void* y;
   uint32_t rows, pool, heads, head_dim, groups, d_state;
-  bool st4;
+  bool vec;  // state rows start at multiples of 16 bytes
 };
 
 struct NormArgs {

@@ -29,6 +29,7 @@ typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 // A matrix operand as the 16x16 tiles take it: lane l holds row (or column)
@@ -145,9 +146,67 @@ __device__ __forceinline__ float load1(const T* p) {
   return (float)*p;
 }
 
+// Global memory as the tile loads and stores see it: a uniform base and byte
+// offsets below 2^31 (clear.cpp holds strides to that).  An access at kAbsent
+// reads zero and writes nothing, so that edges need no branches, which would
+// hold back the loads behind them.
+constexpr uint32_t kAbsent = 0xfffffff0u;
+struct Mem {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ explicit Mem(const void* base)
+      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0x7fffffff, 0x00027000)) {}
+  __device__ __forceinline__ u32x4 load16(uint32_t at) const {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+  }
+  template <typename T>
+  __device__ __forceinline__ uint32_t load_bits(uint32_t at) const {
+    if constexpr (sizeof(T) == 4)
+      return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+    else
+      return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+  }
+  template <typename T>
+  __device__ __forceinline__ float load(uint32_t at) const {
+    const uint32_t w = load_bits<T>(at);
+    return __uint_as_float(sizeof(T) == 4 ? w : w << 16);
+  }
+  // Four neighbouring elements at byte offset `at`, those at or past `left`
+  // absent; whole: all or none, in one access.
+  template <typename T, bool WHOLE>
+  __device__ __forceinline__ void store_four(uint32_t at, const f32x4& v, int left) const {
+    const typename Elem<T>::Four o = to_four<T>(v);
+    if constexpr (WHOLE) {
+      if constexpr (sizeof(T) == 4)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), r,
+                                               left > 0 ? at : kAbsent, 0, 0);
+      else
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, o), r,
+                                              left > 0 ? at : kAbsent, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t to = i < left ? at + i * (uint32_t)sizeof(T) : kAbsent;
+        if constexpr (sizeof(T) == 4)
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(o[i]), r, to, 0, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(s16x4, o)[i], r, to, 0, 0);
+      }
+    }
+  }
+  template <bool WHOLE>
+  __device__ __forceinline__ f32x4 load_four(uint32_t at, int left) const {
+    if constexpr (WHOLE) return __builtin_bit_cast(f32x4, load16(left > 0 ? at : kAbsent));
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = load<float>(i < left ? at + 4 * i : kAbsent);
+    return v;
+  }
+};
+
 // Registers of one thread for a tile of ROWS x COLS elements on its way from
-// global memory to LDS; rows and columns past the valid ones are zero.
-template <typename T, int ROWS, int COLS, int THREADS>
+// global memory to LDS; rows and columns past the valid ones are zero.  VEC:
+// rows start at multiples of 16 bytes.
+template <typename T, int ROWS, int COLS, int THREADS, bool VEC>
 struct Stage {
   static constexpr int kUnit = Elem<T>::kUnit;
   static constexpr int kPerRow = COLS / kUnit;
@@ -155,28 +214,28 @@ struct Stage {
   static_assert(ROWS * kPerRow % THREADS == 0, "whole units per thread");
   u32x4 r[kUnits];
 
-  __device__ __forceinline__ void load(const T* base, int64_t pitch, int rows, int cols,
-                                       bool vec) {
+  __device__ __forceinline__ void load(const T* base, uint32_t pitch, int rows, int cols) {
+    const Mem m(base);
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
       const int i = threadIdx.x + k * THREADS;
       const int row = i / kPerRow, col = i % kPerRow * kUnit;
-      const T* p = base + row * pitch + col;
-      u32x4 v = {0, 0, 0, 0};
-      if (vec) {
-        if (row < rows && col < cols) v = *reinterpret_cast<const u32x4*>(p);
-      } else if (row < rows) {
+      const uint32_t at = (row * pitch + col) * (uint32_t)sizeof(T);
+      if constexpr (VEC) {
+        r[k] = m.load16(row < rows && col < cols ? at : kAbsent);
+      } else {
+        u32x4 v = {0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < kUnit; ++j) {
-          if (col + j < cols) {
-            if constexpr (sizeof(T) == 4)
-              v[j] = *reinterpret_cast<const uint32_t*>(p + j);
-            else
-              v[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + j) << (16 * (j & 1));
-          }
+          const uint32_t w =
+              m.load_bits<T>(row < rows && col + j < cols ? at + j * (uint32_t)sizeof(T) : kAbsent);
+          if constexpr (sizeof(T) == 4)
+            v[j] = w;
+          else
+            v[j / 2] |= w << (16 * (j & 1));
         }
+        r[k] = v;
       }
-      r[k] = v;
     }
   }
   __device__ __forceinline__ void store(T* tile, int pitch) const {
@@ -209,25 +268,6 @@ struct Stage {
   }
 };
 
-// Four neighbouring fp32 (state entries) with those at or past `left` absent.
-__device__ __forceinline__ f32x4 load_four(const float* p, int left, bool whole) {
-  if (whole) return left > 0 ? *reinterpret_cast<const f32x4*>(p) : f32x4{0, 0, 0, 0};
-  f32x4 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = i < left ? p[i] : 0.0f;
-  return v;
-}
-template <typename T>
-__device__ __forceinline__ void store_four(T* p, const f32x4& v, int left, bool whole) {
-  if (whole) {
-    if (left > 0) *reinterpret_cast<typename Elem<T>::Four*>(p) = to_four<T>(v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < left) p[i] = (T)v[i];
-  }
-}
-
 // Running sums of the log decays (base 2) of a chunk, lane l the token l, in
 // fp64 and then as a pair of floats: hi a multiple of 2^-6, so that hi_s - hi_r
 // is exact and a difference of two sums is as accurate as a sum over the
@@ -242,19 +282,29 @@ struct Cum {
 __device__ __forceinline__ float exp2_diff(float hs, float ls, float hr, float lr) {
   return __builtin_amdgcn_exp2f((hs - hr) + (ls - lr));
 }
+// One step of the scan over a wave: adds the value that the DPP control moves
+// here (0 where it moves none).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double c) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, c);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)w, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(w >> 32), CTRL, ROWS, 0xf, false);
+  return c + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ Cum cumulate(float la) {
   constexpr double kLog2e = 1.4426950408889634;
   double c = (double)(la < kReset ? kReset : la) * kLog2e;
-  const int l = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const double o = __shfl_up(c, d);
-    c += l >= d ? o : 0.0;
-  }
+  c = dpp_add<0x111, 0xf>(c);  // row_shr 1, 2, 4, 8: sums within 16 lanes
+  c = dpp_add<0x112, 0xf>(c);
+  c = dpp_add<0x114, 0xf>(c);
+  c = dpp_add<0x118, 0xf>(c);
+  c = dpp_add<0x142, 0xa>(c);  // row_bcast 15 to rows 1 and 3
+  c = dpp_add<0x143, 0xc>(c);  // row_bcast 31 to rows 2 and 3
   Cum r;
   r.hi = (float)(__builtin_rint(c * 64.0) * (1.0 / 64.0));
   r.lo = (float)(c - (double)r.hi);
-  const float th = __shfl(r.hi, 63), tl = __shfl(r.lo, 63);
+  const float th = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_uint(r.hi), 63));
+  const float tl = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_uint(r.lo), 63));
   r.e = exp2_diff(r.hi, r.lo, 0.0f, 0.0f);
   r.w = exp2_diff(th, tl, r.hi, r.lo);
   r.total = __builtin_amdgcn_exp2f(th + tl);
@@ -289,25 +339,26 @@ __device__ __forceinline__ Where where(const ScanShape& sh) {
   return w;
 }
 
-template <int NTILES>
+template <bool VEC, int NTILES>
 __device__ __forceinline__ void load_state(f32x4 (&s)[NTILES], const float* base, int p, int rows,
-                                           int N, bool st4) {
+                                           int N) {
   const int g = (threadIdx.x & 63) >> 4;
+  const Mem m(base);
 #pragma unroll
   for (int t = 0; t < NTILES; ++t) {
     const int n = 16 * t + 4 * g;
-    s[t] = p < rows ? load_four(base + (int64_t)p * N + n, N - n, st4) : f32x4{0, 0, 0, 0};
+    s[t] = m.load_four<VEC>((p * N + n) * 4, p < rows ? N - n : 0);
   }
 }
-template <int NTILES, typename T>
+template <bool VEC, typename T, int NTILES>
 __device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], T* base, int p, int rows,
-                                            int N, bool st4) {
+                                            int N) {
   const int g = (threadIdx.x & 63) >> 4;
-  if (p >= rows) return;
+  const Mem m(base);
 #pragma unroll
   for (int t = 0; t < NTILES; ++t) {
     const int n = 16 * t + 4 * g;
-    store_four<T>(base + (int64_t)p * N + n, s[t], N - n, st4);
+    m.store_four<T, VEC>((p * N + n) * (uint32_t)sizeof(T), s[t], p < rows ? N - n : 0);
   }
 }
 
@@ -341,7 +392,7 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16], const T* xs, c
 // state that enters the segment: the states that enter the chunks, and the
 // final state.  Memory bound: u and v are read once, 4 P N bytes written per
 // segment or one state per chunk.
-template <typename T, int NT>
+template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(256) void k_scan_states(ScanShape sh, ScanDir d0, ScanDir d1,
                                                      bool summaries) {
   constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
@@ -370,29 +421,29 @@ __global__ __launch_bounds__(256) void k_scan_states(ScanShape sh, ScanDir d0, S
                       : d.init       ? d.init + head * size
                                      : nullptr;
   if (from) {
-    load_state(s, from + (uint64_t)p0 * N, p, rows, N, sh.st4);
+    load_state<VEC>(s, from + (uint64_t)p0 * N, p, rows, N);
   } else {
 #pragma unroll
     for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
   }
-  Stage<T, Q, PT, 256> xst;
-  Stage<T, Q, NT, 256> bst;
+  Stage<T, Q, PT, 256, VEC> xst;
+  Stage<T, Q, NT, 256, VEC> bst;
   float lav = 0.0f;
   auto fetch = [&](int k) {
     const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
     const int64_t t0 = (int64_t)c * Q;
     const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    xst.load(u + t0 * d.u_token, d.u_token, n, rows, sh.vec);
-    bst.load(v + t0 * d.v_token, d.v_token, n, N, sh.vec);
-    lav = lane < n ? load1(la + (t0 + lane) * sh.la_token) : 0.0f;
+    lav = Mem(la + t0 * sh.la_token)
+              .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
+    xst.load(u + t0 * d.u_token, d.u_token, n, rows);
+    bst.load(v + t0 * d.v_token, d.v_token, n, N);
   };
   fetch(0);
   float decay = 1.0f;
   for (int k = 0; k < count; ++k) {
     if (d.chunk_states && !summaries) {
       const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
-      store_state(s, (T*)d.chunk_states + (head * sh.chunks + c) * size + (uint64_t)p0 * N, p,
-                  rows, N, sh.st4);
+      store_state<VEC>(s, (T*)d.chunk_states + (head * sh.chunks + c) * size + (uint64_t)p0 * N, p, rows, N);
     }
     Cum cum;
     if (wave == 0) cum = cumulate(lav);
@@ -409,11 +460,10 @@ __global__ __launch_bounds__(256) void k_scan_states(ScanShape sh, ScanDir d0, S
     decay *= total;
   }
   if (summaries) {
-    store_state(s, d.seg_states + (head * sh.segs + at.seg + 1) * size + (uint64_t)p0 * N, p, rows,
-                N, sh.st4);
+    store_state<VEC>(s, d.seg_states + (head * sh.segs + at.seg + 1) * size + (uint64_t)p0 * N, p, rows, N);
     if (threadIdx.x == 0 && at.pt == 0) d.seg_decay[head * sh.segs + at.seg] = decay;
   } else if (d.fin && at.seg + 1 == sh.segs) {
-    store_state(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N, sh.st4);
+    store_state<VEC>(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N);
   }
 }
 
@@ -437,7 +487,7 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
 }
 
 // Outputs and final state.
-template <typename T, int NT>
+template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(256) void k_scan_out(ScanShape sh, ScanDir d, ScanOut o) {
   constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
   __shared__ __align__(16) T xs[Q * XS];
@@ -467,21 +517,22 @@ __global__ __launch_bounds__(256) void k_scan_out(ScanShape sh, ScanDir d, ScanO
                       : d.init     ? d.init + head * size
                                    : nullptr;
   if (from) {
-    load_state(s, from + (uint64_t)p0 * N, p, rows, N, sh.st4);
+    load_state<VEC>(s, from + (uint64_t)p0 * N, p, rows, N);
   } else {
 #pragma unroll
     for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
   }
-  Stage<T, Q, PT, 256> xst;
-  Stage<T, Q, NT, 256> bst, cst;
+  Stage<T, Q, PT, 256, VEC> xst;
+  Stage<T, Q, NT, 256, VEC> bst, cst;
   float lav = 0.0f;
   auto fetch = [&](int k) {
     const int64_t t0 = (int64_t)(first + k) * Q;
     const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    xst.load(u + t0 * d.u_token, d.u_token, n, rows, sh.vec);
-    bst.load(v + t0 * d.v_token, d.v_token, n, N, sh.vec);
-    cst.load(cc + t0 * o.c_token, o.c_token, n, N, sh.vec);
-    lav = lane < n ? load1(la + (t0 + lane) * sh.la_token) : 0.0f;
+    lav = Mem(la + t0 * sh.la_token)
+              .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
+    xst.load(u + t0 * d.u_token, d.u_token, n, rows);
+    bst.load(v + t0 * d.v_token, d.v_token, n, N);
+    cst.load(cc + t0 * o.c_token, o.c_token, n, N);
   };
   fetch(0);
   for (int k = 0; k < count; ++k) {
@@ -531,7 +582,10 @@ __global__ __launch_bounds__(256) void k_scan_out(ScanShape sh, ScanDir d, ScanO
     }
     // y^T: rows p = 16 t + 4 g + i, column s
     const float es = ec[16 * wave + col];
-    const int64_t ts = (int64_t)(first + k) * Q + 16 * wave + col;
+    const int64_t t0 = (int64_t)(first + k) * Q;
+    const Mem ym(y + t0 * sh.heads * P);
+    const uint32_t yat = (16 * wave + col) * sh.heads * P * (uint32_t)sizeof(T);
+    const bool here = t0 + 16 * wave + col < (int64_t)sh.len;
 #pragma unroll
     for (int t = 0; t < PT / 16; ++t) {
       f32x4 acc = {0, 0, 0, 0};
@@ -548,13 +602,12 @@ __global__ __launch_bounds__(256) void k_scan_out(ScanShape sh, ScanDir d, ScanO
         }
       }
       const int pp = 16 * t + 4 * g;
-      if (ts < (int64_t)sh.len)
-        store_four<T>(y + ts * sh.heads * P + pp, acc, rows - pp, sh.ch4);
+      ym.store_four<T, VEC>(yat + pp * (uint32_t)sizeof(T), acc, here ? rows - pp : 0);
     }
     update_state<T, NT>(s, xs, bs, wt, total, wave);
   }
   if (d.fin && at.seg + 1 == sh.segs)
-    store_state(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N, sh.st4);
+    store_state<VEC>(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N);
 }
 
 // ------------------------------------------------------------ gradient
@@ -571,7 +624,7 @@ __global__ __launch_bounds__(256) void k_scan_out(ScanShape sh, ScanDir d, ScanO
 // The first sum of dla falls from t to t + 1 by row sum minus column sum of
 // D K G at t.  Waves 0..3 hold the 16 columns r of G, K and W and form dx;
 // waves 4..7 hold 16 tokens of dC and dB.
-template <typename T, int NT>
+template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
   __shared__ __align__(16) T bs[Q * NS];
@@ -598,29 +651,27 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   const uint64_t size = (uint64_t)P * N;
 
   {
-    Stage<T, Q, NT, 512> st;
-    st.load((const T*)a.b + b * a.b_batch + t0 * a.b_token + (int64_t)grp * N, a.b_token, n, N,
-            sh.vec);
+    Stage<T, Q, NT, 512, VEC> st;
+    st.load((const T*)a.b + b * a.b_batch + t0 * a.b_token + (int64_t)grp * N, a.b_token, n, N);
     st.store(bs, NS);
-    st.load((const T*)a.c + b * a.c_batch + t0 * a.c_token + (int64_t)grp * N, a.c_token, n, N,
-            sh.vec);
+    st.load((const T*)a.c + b * a.c_batch + t0 * a.c_token + (int64_t)grp * N, a.c_token, n, N);
     st.store(cs, NS);
   }
-  Stage<T, Q, PT, 512> xst, dyst;
-  Stage<T, PT, NT, 512> sst, rst;
+  Stage<T, Q, PT, 512, VEC> xst, dyst;
+  Stage<T, PT, NT, 512, VEC> sst, rst;
   float lav = 0.0f;
   auto fetch = [&](uint32_t k) {  // k: head of the split and channel tile
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
     const int p0 = pt * PT, rows = min(PT, P - p0);
+    lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h)
+              .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
     xst.load((const T*)a.x + b * a.x_batch + t0 * a.x_token + (int64_t)h * P + p0, a.x_token, n,
-             rows, sh.vec);
+             rows);
     dyst.load((const T*)a.dy + b * a.dy_batch + t0 * a.dy_token + (int64_t)h * P + p0, a.dy_token,
-              n, rows, sh.vec);
+              n, rows);
     const uint64_t at = (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size + (uint64_t)p0 * N;
-    sst.load((const T*)a.s_in + at, N, rows, N, sh.vec);
-    rst.load((const T*)a.r_in + at, N, rows, N, sh.vec);
-    lav = lane < n ? load1((const T*)sh.la + b * sh.la_batch + (t0 + lane) * sh.la_token + h)
-                   : 0.0f;
+    sst.load((const T*)a.s_in + at, N, rows, N);
+    rst.load((const T*)a.r_in + at, N, rows, N);
   };
   fetch(0);
   __syncthreads();
@@ -734,8 +785,8 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
 #pragma unroll
       for (int q = 0; q < NT / 32; ++q)
         bf[q] = row_frag(bs + (16 * tile + col) * NS + 32 * q + 8 * g);
-      const int64_t t = t0 + 16 * tile + col;
-      T* dx = (T*)a.dx + (((uint64_t)b * sh.len + t) * sh.heads + h) * P + p0;
+      const Mem dx((T*)a.dx + (((uint64_t)b * sh.len + t0) * sh.heads + h) * P + p0);
+      const uint32_t at = (16 * tile + col) * sh.heads * P * (uint32_t)sizeof(T);
 #pragma unroll
       for (int x = 0; x < PT / 16; ++x) {
         f32x4 acc = {0, 0, 0, 0};
@@ -752,7 +803,8 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
           }
         }
         const int pp = 16 * x + 4 * g;
-        if (t < (int64_t)sh.len) store_four<T>(dx + pp, acc, rows - pp, sh.ch4);
+        dx.store_four<T, VEC>(at + pp * (uint32_t)sizeof(T), acc,
+                              16 * tile + col < n ? rows - pp : 0);
       }
     } else {
       const float wr = wt[16 * tile + col];
@@ -809,9 +861,10 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   }
   __syncthreads();
   if (left) return;
-  const int64_t t = t0 + 16 * tile + col;
-  const uint64_t row = (((uint64_t)b * sh.len + t) * sh.groups + grp) * N;
+  const uint64_t row = (((uint64_t)b * sh.len + t0) * sh.groups + grp) * N;
   const uint64_t part = (uint64_t)split * sh.batch * sh.len * sh.groups * N + row;
+  const Mem dcm(a.dc_part ? (void*)(a.dc_part + part) : (void*)((T*)a.dc + row));
+  const Mem dbm(a.db_part ? (void*)(a.db_part + part) : (void*)((T*)a.db + row));
   Frag wc[2], wb[2];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
@@ -829,14 +882,14 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
                        col_four(cs, NS, 32 * q + 8 * g + 4, 16 * x)), wb[q], db[x]);
     }
     const int nn = 16 * x + 4 * g;
-    if (t < (int64_t)sh.len) {
-      if (a.db_part) {
-        store_four<float>(a.dc_part + part + nn, dc[x], N - nn, sh.st4);
-        store_four<float>(a.db_part + part + nn, db[x], N - nn, sh.st4);
-      } else {
-        store_four<T>((T*)a.dc + row + nn, dc[x], N - nn, sh.st4);
-        store_four<T>((T*)a.db + row + nn, db[x], N - nn, sh.st4);
-      }
+    const uint32_t at = (16 * tile + col) * sh.groups * N + nn;
+    const int some = 16 * tile + col < n ? N - nn : 0;
+    if (a.db_part) {
+      dcm.store_four<float, VEC>(at * 4, dc[x], some);
+      dbm.store_four<float, VEC>(at * 4, db[x], some);
+    } else {
+      dcm.store_four<T, VEC>(at * (uint32_t)sizeof(T), dc[x], some);
+      dbm.store_four<T, VEC>(at * (uint32_t)sizeof(T), db[x], some);
     }
   }
 }
@@ -857,7 +910,7 @@ __global__ __launch_bounds__(256) void k_scan_parts(ScanGrad a, uint64_t count) 
 // One served token per row: S = e^{la} S + x B^T in place, y = S C.  Memory
 // bound by the state, which is read and written once.  LPR lanes share one
 // state row, four entries each.
-template <typename T, int LPR>
+template <typename T, int LPR, bool VEC>
 __global__ __launch_bounds__(256) void k_scan_step(StepArgs a, uint32_t psplit) {
   constexpr int kRows = 256 / LPR;  // state rows per pass of the workgroup
   const uint32_t ps = blockIdx.x % psplit;
@@ -884,14 +937,13 @@ __global__ __launch_bounds__(256) void k_scan_step(StepArgs a, uint32_t psplit) 
     b[i] = n + i < N ? load1(bp + i) : 0.0f;
     c[i] = n + i < N ? load1(cp + i) : 0.0f;
   }
-  float* s = a.state + ((uint64_t)slot * a.heads + h) * P * N + n;
+  const Mem s(a.state + ((uint64_t)slot * a.heads + h) * P * N);
   for (int p = ps * kRows + sub; p < P; p += psplit * kRows) {
-    float* sp = s + (int64_t)p * N;
-    f32x4 v = load_four(sp, N - n, a.st4);
+    f32x4 v = s.load_four<VEC>((p * N + n) * 4, N - n);
     const float xv = load1(x + p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(decay, v[i], xv * b[i]);
-    store_four<float>(sp, v, N - n, a.st4);
+    s.store_four<float, VEC>((p * N + n) * 4, v, N - n);
     float d = (v[0] * c[0] + v[1] * c[1]) + (v[2] * c[2] + v[3] * c[3]);
 #pragma unroll
     for (int k = 1; k < LPR; k *= 2) d += __shfl_xor(d, k);
@@ -904,52 +956,54 @@ __global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to
   if (i < count) to[i] = from ? from[i] : 0.0f;
 }
 
-template <typename T, int NT>
+template <typename T, int NT, bool VEC>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
   const ScanDir &d0 = d[0], &d1 = d[nd - 1];
   const dim3 grid(sh.batch * sh.segs * sh.heads * sh.ptiles, 1, nd);
   if (sh.segs > 1) {
-    k_scan_states<T, NT><<<grid, 256, 0, s>>>(sh, d0, d1, true);
+    k_scan_states<T, NT, VEC><<<grid, 256, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
     const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
     k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
     if (hipError_t e = hipGetLastError()) return e;
   }
   if (!main) return hipSuccess;
-  k_scan_states<T, NT><<<grid, 256, 0, s>>>(sh, d0, d1, false);
+  k_scan_states<T, NT, VEC><<<grid, 256, 0, s>>>(sh, d0, d1, false);
   return hipGetLastError();
 }
 
-// One instance per element type and padded state size.
-#define FESC_SCAN_CASES(DTYPE, N, CALL)                      \
-  ((DTYPE) == FESC_BF16 ? ((N) <= 64 ? CALL(__bf16, 64) : CALL(__bf16, 128)) \
-                        : ((N) <= 64 ? CALL(float, 64) : CALL(float, 128)))
+// One instance per element type, padded state size and alignment.
+#define FESC_SCAN_N(T, SH, CALL)                                                 \
+  ((SH).d_state <= 64 ? ((SH).vec ? CALL(T, 64, true) : CALL(T, 64, false))      \
+                      : ((SH).vec ? CALL(T, 128, true) : CALL(T, 128, false)))
+#define FESC_SCAN_CASES(DTYPE, SH, CALL) \
+  ((DTYPE) == FESC_BF16 ? FESC_SCAN_N(__bf16, SH, CALL) : FESC_SCAN_N(float, SH, CALL))
 
 }  // namespace
 
 hipError_t launch_scan_states(uint32_t dtype, const ScanShape& sh, const ScanDir* d, int nd,
                               hipStream_t s) {
-#define CALL(T, NT) states<T, NT>(sh, d, nd, true, s)
-  return FESC_SCAN_CASES(dtype, sh.d_state, CALL);
+#define CALL(T, NT, VEC) states<T, NT, VEC>(sh, d, nd, true, s)
+  return FESC_SCAN_CASES(dtype, sh, CALL);
 #undef CALL
 }
 
 hipError_t launch_scan_out(uint32_t dtype, const ScanShape& sh, const ScanDir& d,
                            const ScanOut& o, hipStream_t s) {
-#define CALL(T, NT) states<T, NT>(sh, &d, 1, false, s)
-  if (hipError_t e = FESC_SCAN_CASES(dtype, sh.d_state, CALL)) return e;
+#define CALL(T, NT, VEC) states<T, NT, VEC>(sh, &d, 1, false, s)
+  if (hipError_t e = FESC_SCAN_CASES(dtype, sh, CALL)) return e;
 #undef CALL
   const uint32_t grid = sh.batch * sh.segs * sh.heads * sh.ptiles;
-#define CALL(T, NT) (k_scan_out<T, NT><<<grid, 256, 0, s>>>(sh, d, o), hipGetLastError())
-  return FESC_SCAN_CASES(dtype, sh.d_state, CALL);
+#define CALL(T, NT, VEC) (k_scan_out<T, NT, VEC><<<grid, 256, 0, s>>>(sh, d, o), hipGetLastError())
+  return FESC_SCAN_CASES(dtype, sh, CALL);
 #undef CALL
 }
 
 hipError_t launch_scan_grad(uint32_t dtype, const ScanShape& sh, const ScanGrad& g,
                             hipStream_t s) {
   const dim3 grid(sh.batch * sh.chunks, sh.groups * g.splits);
-#define CALL(T, NT) (k_scan_grad<T, NT><<<grid, 512, 0, s>>>(sh, g), hipGetLastError())
-  hipError_t e = FESC_SCAN_CASES(dtype, sh.d_state, CALL);
+#define CALL(T, NT, VEC) (k_scan_grad<T, NT, VEC><<<grid, 512, 0, s>>>(sh, g), hipGetLastError())
+  hipError_t e = FESC_SCAN_CASES(dtype, sh, CALL);
 #undef CALL
   if (e || g.splits == 1) return e;
   const uint64_t count = (uint64_t)sh.batch * sh.len * sh.groups * sh.d_state;
@@ -968,15 +1022,23 @@ hipError_t launch_scan_step(uint32_t dtype, const StepArgs& a, hipStream_t s) {
   // a few rows only: one pass per workgroup, so that all compute units work
   const uint32_t psplit = heads >= 2048 ? 1 : passes;
   const uint32_t grid = (uint32_t)(heads * psplit);
-#define STEP(T)                                                       \
-  if (lpr == 16)                                                      \
-    k_scan_step<T, 16><<<grid, 256, 0, s>>>(a, psplit);               \
-  else                                                                \
-    k_scan_step<T, 32><<<grid, 256, 0, s>>>(a, psplit)
+#define STEP(T, LPR)                                                 \
+  if (a.vec)                                                         \
+    k_scan_step<T, LPR, true><<<grid, 256, 0, s>>>(a, psplit);       \
+  else                                                               \
+    k_scan_step<T, LPR, false><<<grid, 256, 0, s>>>(a, psplit)
   if (dtype == FESC_BF16) {
-    STEP(__bf16);
+    if (lpr == 16) {
+      STEP(__bf16, 16);
+    } else {
+      STEP(__bf16, 32);
+    }
   } else {
-    STEP(float);
+    if (lpr == 16) {
+      STEP(float, 16);
+    } else {
+      STEP(float, 32);
+    }
   }
 #undef STEP
   return hipGetLastError();

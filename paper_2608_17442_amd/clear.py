@@ -58,15 +58,17 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(t):
-    """The current stream of t's device, as its handle."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+def _stream(device):
+    """The current stream of a device, as its handle."""
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _once():
     if torch.is_grad_enabled():
         raise RuntimeError("the block in the clear is differentiable once: no create_graph=True")
 
+
+# ---------------------------------------------------------- argument checks
 
 def _tensor(t, what, like=None, dtype=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -82,7 +84,6 @@ def _tensor(t, what, like=None, dtype=None):
             raise TypeError(f"{what}: expected {dtype or like.dtype}, got {t.dtype}")
         if t.device != like.device:
             raise ValueError(f"{what}: on {t.device}, expected {like.device}")
-    return t
 
 
 def _shape(t, shape, what):
@@ -104,7 +105,6 @@ def _dense_tail(t, dims):
 def _factor(t, dims, what):
     if t.numel() and not _dense_tail(t, dims):
         raise ValueError(f"{what}: the last {dims} dimension(s) must be contiguous")
-    return t
 
 
 def _state(t, shape, what, like):
@@ -112,48 +112,103 @@ def _state(t, shape, what, like):
     _shape(t, shape, what)
     if not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous")
-    return t
 
 
-def _space(desc, query, *args):
+# A call's plan: its checked descriptor and workspace sizes, kept by what they
+# follow from (types, shapes, strides, device) so that a program that makes
+# the same kind of call again does not check it again.
+_PLANS = {}
+_MOST_PLANS = 4096
+
+
+def _plan(key, make, args):
+    plan = _PLANS.get(key)
+    if plan is None:
+        plan = make(*args)
+        if len(_PLANS) >= _MOST_PLANS:
+            _PLANS.clear()
+        _PLANS[key] = plan
+    return plan
+
+
+def _key(name, *ts):
+    """What a plan follows from; no plan is kept for what is not a tensor."""
+    if not isinstance(ts[0], torch.Tensor) or not ts[0].is_cuda:
+        raise TypeError(f"{name}: expected CUDA tensors")
+    key = [name, torch.cuda.current_device()]
+    for t in ts:
+        if t is None:
+            key.append(None)
+        else:
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name}: expected tensors, got {type(t).__name__}")
+            key += (t.dtype, t.device, t.shape, t.stride())
+    return tuple(key)
+
+
+class _Plan:
+    """ref: the descriptor's address; device; workspace sizes, forward and
+    backward."""
+
+    __slots__ = ("desc", "ref", "device", "space", "grad_space", "shapes")
+
+    def __init__(self, desc, device):
+        self.desc, self.ref, self.device = desc, ctypes.byref(desc), device
+
+
+def _space(query, *args):
     need = _sz()
-    _check(query(ctypes.byref(desc), *args, ctypes.byref(need)))
+    _check(query(*args, ctypes.byref(need)))
     return need.value
 
 
-def _buffer(bytes_, like):
-    return torch.empty(bytes_, dtype=torch.uint8, device=like.device) if bytes_ else None
+def _buffer(size, device):
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
 
 
 # ---------------------------------------------------------------- recurrence
 
-def _scan_desc(x, la, B, C):
+def _scan_plan(x, la, B, C, h0, dy=None):
+    _tensor(x, "x")
+    for t, what in ((la, "la"), (B, "B"), (C, "C")):
+        _tensor(t, what, x)
+    if x.dim() != 4 or B.dim() != 4:
+        raise ValueError("x, B: expected [batch, len, heads or groups, width]")
+    _shape(la, x.shape[:3], "la")
+    _shape(B, (*x.shape[:2], *B.shape[2:]), "B")
+    _shape(C, B.shape, "C")
+    _factor(x, 2, "x"), _factor(la, 1, "la"), _factor(B, 2, "B"), _factor(C, 2, "C")
     b, n, H, P = x.shape
     G, N = B.shape[2:]
-    return _ScanDesc(_TYPES[x.dtype], b, n, H, P, G, N, x.stride(1), x.stride(0), la.stride(1),
-                     la.stride(0), B.stride(1), B.stride(0), C.stride(1), C.stride(0), 0, 0)
+    if h0 is not None:
+        _state(h0, (b, H, P, N), "h0", x)
+    d = _ScanDesc(_TYPES[x.dtype], b, n, H, P, G, N, x.stride(1), x.stride(0), la.stride(1),
+                  la.stride(0), B.stride(1), B.stride(0), C.stride(1), C.stride(0),
+                  dy.stride(1) if dy is not None else 0, dy.stride(0) if dy is not None else 0)
+    plan = _Plan(d, x.device)
+    plan.space = _space(_lib.fesc_clear_scan_workspace, plan.ref, 0)
+    plan.grad_space = _space(_lib.fesc_clear_scan_workspace, plan.ref, 1) if dy is not None else 0
+    plan.shapes = (tuple(x.shape), (b, H, P, N))
+    return plan
 
 
-def _scan_forward(x, la, B, C, h0, want_state):
-    d = _scan_desc(x, la, B, C)
-    b, n, H, P = x.shape
-    y = torch.empty((b, n, H, P), dtype=x.dtype, device=x.device)
-    h = None
-    if want_state:
-        h = torch.empty((b, H, P, B.shape[3]), dtype=torch.float32, device=x.device)
-    need = _space(d, _lib.fesc_clear_scan_workspace, 0)
-    w = _buffer(need, x)
-    _check(_lib.fesc_clear_scan(ctypes.byref(d), _p(x), _p(la), _p(B), _p(C), _p(h0), _p(y),
-                                _p(h), _p(w), need, _stream(x)))
+def _scan_forward(plan, x, la, B, C, h0, want_state):
+    device = plan.device
+    y = torch.empty(plan.shapes[0], dtype=x.dtype, device=device)
+    h = torch.empty(plan.shapes[1], dtype=torch.float32, device=device) if want_state else None
+    w = _buffer(plan.space, device)
+    _check(_lib.fesc_clear_scan(plan.ref, x.data_ptr(), la.data_ptr(), B.data_ptr(), C.data_ptr(),
+                                _p(h0), y.data_ptr(), _p(h), _p(w), plan.space,
+                                _stream(device.index)))
     return y, h
 
 
 class _Scan(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, la, B, C, h0, want_state):
+    def forward(ctx, x, la, B, C, h0, want_state, plan):
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(x, la, B, C, h0)
-        y, h = _scan_forward(x, la, B, C, h0, want_state)
+        y, h = _scan_forward(plan, x, la, B, C, h0, want_state)
         return (y, h) if want_state else y
 
     @staticmethod
@@ -162,26 +217,25 @@ class _Scan(torch.autograd.Function):
         x, la, B, C, h0 = ctx.saved_tensors
         if dy is None:
             if dh is None:
-                return (None,) * 6
+                return (None,) * 7
             dy = torch.zeros_like(x, memory_format=torch.contiguous_format)
         elif not _dense_tail(dy, 2):
             dy = dy.contiguous()
         if dh is not None:
             dh = dh.contiguous()
-        d = _scan_desc(x, la, B, C)
-        d.dy_token, d.dy_batch = dy.stride(1), dy.stride(0)
+        plan = _plan(_key("scan gradient", x, la, B, C, h0, dy), _scan_plan, (x, la, B, C, h0, dy))
 
         def like(t):
-            return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+            return torch.empty(t.shape, dtype=t.dtype, device=plan.device)
 
         dx, dla, db, dc = like(x), like(la), like(B), like(C)
         dh0 = like(h0) if h0 is not None and ctx.needs_input_grad[4] else None
-        need = _space(d, _lib.fesc_clear_scan_workspace, 1)
-        w = _buffer(need, x)
+        w = _buffer(plan.grad_space, plan.device)
         _check(_lib.fesc_clear_scan_bwd(
-            ctypes.byref(d), _p(x), _p(la), _p(B), _p(C), _p(h0), _p(dy), _p(dh), _p(dx), _p(dla),
-            _p(db), _p(dc), _p(dh0), _p(w), need, _stream(x)))
-        return dx, dla, db, dc, dh0, None
+            plan.ref, x.data_ptr(), la.data_ptr(), B.data_ptr(), C.data_ptr(), _p(h0),
+            dy.data_ptr(), _p(dh), dx.data_ptr(), dla.data_ptr(), db.data_ptr(), dc.data_ptr(),
+            _p(dh0), _p(w), plan.grad_space, _stream(plan.device.index)))
+        return dx, dla, db, dc, dh0, None, None
 
 
 def scan(x, la, B, C, h0=None, return_state=False, stream=None):
@@ -192,42 +246,21 @@ def scan(x, la, B, C, h0=None, return_state=False, stream=None):
     -inf resets the state), B and C [batch, len, groups, d_state]; the first
     two dimensions may have any strides, so slices of a wider projection do.
     h0 and the returned state: float32 [batch, heads, head_dim, d_state].
-    Differentiable with respect to all five.
+    Differentiable (once) with respect to all five.
     """
     if stream is not None:
         with torch.cuda.stream(stream):
             return scan(x, la, B, C, h0, return_state)
-    _tensor(x, "x")
-    for t, what in ((la, "la"), (B, "B"), (C, "C")):
-        _tensor(t, what, x)
-    if x.dim() != 4 or B.dim() != 4:
-        raise ValueError("x, B: expected [batch, len, heads or groups, width]")
-    _shape(la, x.shape[:3], "la")
-    _shape(B, (*x.shape[:2], *B.shape[2:]), "B")
-    _shape(C, B.shape, "C")
-    _factor(x, 2, "x"), _factor(la, 1, "la"), _factor(B, 2, "B"), _factor(C, 2, "C")
-    if h0 is not None:
-        _state(h0, (x.shape[0], *x.shape[2:], B.shape[3]), "h0", x)
+    plan = _plan(_key("scan", x, la, B, C, h0), _scan_plan, (x, la, B, C, h0))
     if torch.is_grad_enabled() and (x.requires_grad or la.requires_grad or B.requires_grad
                                     or C.requires_grad
                                     or (h0 is not None and h0.requires_grad)):
-        return _Scan.apply(x, la, B, C, h0, return_state)
-    y, h = _scan_forward(x, la, B, C, h0, return_state)
+        return _Scan.apply(x, la, B, C, h0, return_state, plan)
+    y, h = _scan_forward(plan, x, la, B, C, h0, return_state)
     return (y, h) if return_state else y
 
 
-def scan_step(x, la, B, C, state, slots=None, stream=None):
-    """One token for each row: updates `state` in place and returns y
-    [rows, heads, head_dim].
-
-    x [rows, heads, head_dim], la [rows, heads], B and C [rows, groups,
-    d_state]; state float32 [pool, heads, head_dim, d_state].  Row i uses state
-    slots[i] (int32, None: i); a slot outside the pool (-1) marks an idle row,
-    whose y is zero.  No two rows may name one slot.  Not differentiable.
-    """
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return scan_step(x, la, B, C, state, slots)
+def _step_plan(x, la, B, C, state, slots):
     _tensor(x, "x")
     for t, what in ((la, "la"), (B, "B"), (C, "C")):
         _tensor(t, what, x)
@@ -245,13 +278,34 @@ def scan_step(x, la, B, C, state, slots=None, stream=None):
         _shape(slots, (rows,), "slots")
         if not slots.is_contiguous():
             raise ValueError("slots: must be contiguous")
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, la, B, C, state)):
+    plan = _Plan(_ScanDesc(_TYPES[x.dtype], rows, 1, H, P, G, N, 0, x.stride(0), 0, la.stride(0),
+                           0, B.stride(0), 0, C.stride(0), 0, 0), x.device)
+    plan.shapes = (rows, H, P)
+    return plan
+
+
+def scan_step(x, la, B, C, state, slots=None, stream=None):
+    """One token for each row: updates `state` in place and returns y
+    [rows, heads, head_dim].
+
+    x [rows, heads, head_dim], la [rows, heads], B and C [rows, groups,
+    d_state]; state float32 [pool, heads, head_dim, d_state].  Row i uses state
+    slots[i] (int32, None: i); a slot outside the pool (-1) marks an idle row,
+    whose y is zero.  No two rows may name one slot.  Not differentiable.
+    """
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return scan_step(x, la, B, C, state, slots)
+    plan = _plan(_key("scan_step", x, la, B, C, state, slots), _step_plan,
+                 (x, la, B, C, state, slots))
+    if torch.is_grad_enabled() and (x.requires_grad or la.requires_grad or B.requires_grad
+                                    or C.requires_grad or state.requires_grad):
         raise ValueError("scan_step is not differentiable: use scan, or torch.no_grad()")
-    y = torch.empty((rows, H, P), dtype=x.dtype, device=x.device)
-    d = _ScanDesc(_TYPES[x.dtype], rows, 1, H, P, G, N, 0, x.stride(0), 0, la.stride(0), 0,
-                  B.stride(0), 0, C.stride(0), 0, 0)
-    _check(_lib.fesc_clear_scan_step(ctypes.byref(d), _p(x), _p(la), _p(B), _p(C), _p(state),
-                                     state.shape[0], _p(slots), _p(y), _stream(x)))
+    device = plan.device
+    y = torch.empty(plan.shapes, dtype=x.dtype, device=device)
+    _check(_lib.fesc_clear_scan_step(plan.ref, x.data_ptr(), la.data_ptr(), B.data_ptr(),
+                                     C.data_ptr(), state.data_ptr(), state.shape[0], _p(slots),
+                                     y.data_ptr(), _stream(device.index)))
     return y
 
 
@@ -276,120 +330,134 @@ def _rows(t, what):
     return w if stride is None else stride
 
 
-def _grad_rows(t):
-    """A gradient as rows that lie evenly, with their stride."""
+def _even(t):
+    """A gradient whose rows lie evenly."""
     try:
-        return t, _rows(t, "")
+        _rows(t, "")
+        return t
     except ValueError:
-        t = t.contiguous()
-        return t, t.shape[-1]
+        return t.contiguous()
 
 
-def _norm_desc(t, eps, **strides):
-    w = t.shape[-1]
-    d = _NormDesc(_TYPES[t.dtype], w, t.numel() // w if w else 0, eps)
-    for k, v in strides.items():
-        setattr(d, k, v)
-    return d
-
-
-def _norm_check(first, others, vectors):
-    """Types and shapes of a norm's arrays (name, tensor) and weight vectors."""
-    t = _tensor(first[1], first[0])
-    if t.dim() == 0:
-        raise ValueError(f"{first[0]}: expected [..., width]")
-    for what, o in others:
-        _shape(_tensor(o, what, t), t.shape, what)
+def _norm_plan(arrays, vectors, eps, grads=()):
+    """From (name, tensor) pairs: the row arrays, the weight vectors, and the
+    incoming gradients by the names of their strides (absent: None)."""
+    what, first = arrays[0]
+    _tensor(first, what)
+    if first.dim() == 0:
+        raise ValueError(f"{what}: expected [..., width]")
+    for what, t in arrays[1:]:
+        _tensor(t, what, first)
+        _shape(t, first.shape, what)
     for what, v in vectors:
-        _shape(_tensor(v, what, t), t.shape[-1:], what)
+        _tensor(v, what, first)
+        _shape(v, first.shape[-1:], what)
         if not v.is_contiguous():
             raise ValueError(f"{what}: must be contiguous")
+    w = first.shape[-1]
+    d = _NormDesc(_TYPES[first.dtype], w, first.numel() // w if w else 0, eps)
+    for what, t in arrays:
+        setattr(d, what + "_row", _rows(t, what))
+    for what, t in grads:
+        setattr(d, what + "_row", _rows(t, what) if t is not None else 0)
+    plan = _Plan(d, first.device)
+    plan.grad_space = _space(_lib.fesc_clear_norm_workspace, plan.ref)
+    plan.shapes = tuple(first.shape)
+    return plan
 
 
-def _empty(t):
-    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+def _gated_plan(m, x, z, skip, w, eps, *du):
+    return _norm_plan((("m", m), ("x", x), ("z", z)), (("skip", skip), ("w", w)), eps,
+                      tuple(zip(("du",), du)))
 
 
-def _gated_forward(m, x, z, skip, w, eps):
-    d = _norm_desc(m, eps, m_row=_rows(m, "m"), x_row=_rows(x, "x"), z_row=_rows(z, "z"))
-    u = _empty(m)
-    _check(_lib.fesc_clear_norm_gated(ctypes.byref(d), _p(m), _p(x), _p(z), _p(skip), _p(w), _p(u),
-                                      _stream(m)))
+def _gated_forward(plan, m, x, z, skip, w):
+    u = torch.empty(plan.shapes, dtype=m.dtype, device=plan.device)
+    _check(_lib.fesc_clear_norm_gated(plan.ref, m.data_ptr(), x.data_ptr(), z.data_ptr(),
+                                      skip.data_ptr(), w.data_ptr(), u.data_ptr(),
+                                      _stream(plan.device.index)))
     return u
 
 
 class _Gated(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, m, x, z, skip, w, eps):
+    def forward(ctx, m, x, z, skip, w, eps, plan):
         ctx.eps = eps
         ctx.save_for_backward(m, x, z, skip, w)
-        return _gated_forward(m, x, z, skip, w, eps)
+        return _gated_forward(plan, m, x, z, skip, w)
 
     @staticmethod
     def backward(ctx, du):
         _once()
-        m, x, z, skip, w = ctx.saved_tensors
-        du, du_row = _grad_rows(du)
-        d = _norm_desc(m, ctx.eps, m_row=_rows(m, "m"), x_row=_rows(x, "x"), z_row=_rows(z, "z"),
-                       du_row=du_row)
-        dm, dx, dz, dskip, dw = (_empty(t) for t in (m, x, z, skip, w))
-        need = _space(d, _lib.fesc_clear_norm_workspace)
-        ws = _buffer(need, m)
+        saved = m, x, z, skip, w = ctx.saved_tensors
+        du = _even(du)
+        plan = _plan((ctx.eps, _key("gated gradient", *saved, du)), _gated_plan,
+                     (*saved, ctx.eps, du))
+        dm, dx, dz, dskip, dw = (torch.empty(t.shape, dtype=t.dtype, device=plan.device)
+                                 for t in saved)
+        ws = _buffer(plan.grad_space, plan.device)
         _check(_lib.fesc_clear_norm_gated_bwd(
-            ctypes.byref(d), _p(m), _p(x), _p(z), _p(skip), _p(w), _p(du), _p(dm), _p(dx), _p(dz),
-            _p(dskip), _p(dw), _p(ws), need, _stream(m)))
-        return dm, dx, dz, dskip, dw, None
+            plan.ref, m.data_ptr(), x.data_ptr(), z.data_ptr(), skip.data_ptr(), w.data_ptr(),
+            du.data_ptr(), dm.data_ptr(), dx.data_ptr(), dz.data_ptr(), dskip.data_ptr(),
+            dw.data_ptr(), _p(ws), plan.grad_space, _stream(plan.device.index)))
+        return dm, dx, dz, dskip, dw, None, None
 
 
 def norm_gated(m, x, z, skip, w, eps=1e-5, stream=None):
     """u = v w / sqrt(mean v^2 + eps) over the last dimension, with
     v = (m + skip x) silu(z): m the recurrence's output, x its input (the skip
     connection), z the gate, all [..., width] with rows of any one stride;
-    skip and w [width].  Differentiable with respect to all five."""
+    skip and w [width].  Differentiable (once) with respect to all five."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return norm_gated(m, x, z, skip, w, eps)
-    _norm_check(("m", m), (("x", x), ("z", z)), (("skip", skip), ("w", w)))
+    plan = _plan((eps, _key("norm_gated", m, x, z, skip, w)), _gated_plan, (m, x, z, skip, w, eps))
     if torch.is_grad_enabled() and (m.requires_grad or x.requires_grad or z.requires_grad
                                     or skip.requires_grad or w.requires_grad):
-        return _Gated.apply(m, x, z, skip, w, eps)
-    return _gated_forward(m, x, z, skip, w, eps)
+        return _Gated.apply(m, x, z, skip, w, eps, plan)
+    return _gated_forward(plan, m, x, z, skip, w)
 
 
-def _residual_forward(o, r, scale, w, eps):
-    d = _norm_desc(o, eps, o_row=_rows(o, "o"), r_row=_rows(r, "r"))
-    new, u = _empty(o), _empty(o)
-    _check(_lib.fesc_clear_norm_residual(ctypes.byref(d), _p(o), _p(r), _p(scale), _p(w), _p(new),
-                                         _p(u), _stream(o)))
+def _residual_plan(o, r, scale, w, eps, *grads):
+    return _norm_plan((("o", o), ("r", r)), (("scale", scale), ("w", w)), eps,
+                      tuple(zip(("dr", "du"), grads)))
+
+
+def _residual_forward(plan, o, r, scale, w):
+    new = torch.empty(plan.shapes, dtype=o.dtype, device=plan.device)
+    u = torch.empty(plan.shapes, dtype=o.dtype, device=plan.device)
+    _check(_lib.fesc_clear_norm_residual(plan.ref, o.data_ptr(), r.data_ptr(), scale.data_ptr(),
+                                         w.data_ptr(), new.data_ptr(), u.data_ptr(),
+                                         _stream(plan.device.index)))
     return new, u
 
 
 class _Residual(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, o, r, scale, w, eps):
+    def forward(ctx, o, r, scale, w, eps, plan):
         ctx.set_materialize_grads(False)
         ctx.eps = eps
         ctx.save_for_backward(o, r, scale, w)
-        return _residual_forward(o, r, scale, w, eps)
+        return _residual_forward(plan, o, r, scale, w)
 
     @staticmethod
     def backward(ctx, dnew, du):
         _once()
-        o, r, scale, w = ctx.saved_tensors
+        saved = o, r, scale, w = ctx.saved_tensors
         if dnew is None and du is None:
-            return (None,) * 5
-        d = _norm_desc(o, ctx.eps, o_row=_rows(o, "o"), r_row=_rows(r, "r"))
-        if du is not None:
-            du, d.du_row = _grad_rows(du)
-        if dnew is not None:
-            dnew, d.dr_row = _grad_rows(dnew)
-        do, dr, dscale, dw = (_empty(t) for t in (o, r, scale, w))
-        need = _space(d, _lib.fesc_clear_norm_workspace)
-        ws = _buffer(need, o)
+            return (None,) * 6
+        du = _even(du) if du is not None else None
+        dnew = _even(dnew) if dnew is not None else None
+        plan = _plan((ctx.eps, _key("residual gradient", *saved, dnew, du)), _residual_plan,
+                     (*saved, ctx.eps, dnew, du))
+        do, dr, dscale, dw = (torch.empty(t.shape, dtype=t.dtype, device=plan.device)
+                              for t in saved)
+        ws = _buffer(plan.grad_space, plan.device)
         _check(_lib.fesc_clear_norm_residual_bwd(
-            ctypes.byref(d), _p(o), _p(r), _p(scale), _p(w), _p(du), _p(dnew), _p(do), _p(dr),
-            _p(dscale), _p(dw), _p(ws), need, _stream(o)))
-        return do, dr, dscale, dw, None
+            plan.ref, o.data_ptr(), r.data_ptr(), scale.data_ptr(), w.data_ptr(), _p(du),
+            _p(dnew), do.data_ptr(), dr.data_ptr(), dscale.data_ptr(), dw.data_ptr(), _p(ws),
+            plan.grad_space, _stream(plan.device.index)))
+        return do, dr, dscale, dw, None, None
 
 
 def norm_residual(o, r, scale, w, eps=1e-5, stream=None):
@@ -397,12 +465,13 @@ def norm_residual(o, r, scale, w, eps=1e-5, stream=None):
     output o, and u = r_new w / sqrt(mean r_new^2 + eps), the next block's
     input.  o and r [..., width] with rows of any one stride; scale and w
     [width].  u is formed from r_new before it is rounded.  Differentiable
-    with respect to all four."""
+    (once) with respect to all four."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return norm_residual(o, r, scale, w, eps)
-    _norm_check(("o", o), (("r", r),), (("scale", scale), ("w", w)))
+    plan = _plan((eps, _key("norm_residual", o, r, scale, w)), _residual_plan,
+                 (o, r, scale, w, eps))
     if torch.is_grad_enabled() and (o.requires_grad or r.requires_grad or scale.requires_grad
                                     or w.requires_grad):
-        return _Residual.apply(o, r, scale, w, eps)
-    return _residual_forward(o, r, scale, w, eps)
+        return _Residual.apply(o, r, scale, w, eps, plan)
+    return _residual_forward(plan, o, r, scale, w)

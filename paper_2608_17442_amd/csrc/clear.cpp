@@ -191,8 +191,8 @@ int norm_bwd(const fesc_clear_norm_desc* d, bool gated, NormArgs n, void* worksp
   if (int rc = fesc_clear_norm_workspace(d, &need)) return rc;
   if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
   n.part = reinterpret_cast<float*>(workspace);
-  n.blocks = norm_grad_blocks(n.rows, n.width);
   n.vec = norm_vec(d, n);
+  n.blocks = norm_grad_blocks(n.rows, n.width, n.vec);
   return hip_check(launch_norm_grad(d->dtype, gated, n, S(stream)), "norm gradient");
 }
 
@@ -364,7 +364,9 @@ int fesc_clear_norm_residual(const fesc_clear_norm_desc* d, const void* o, const
 int fesc_clear_norm_workspace(const fesc_clear_norm_desc* d, size_t* bytes) {
   if (int rc = check_norm(d)) return rc;
   if (!bytes) return fail(FESC_ERR_ARG, "null argument");
-  *bytes = round_up((size_t)norm_grad_blocks(d->rows, d->width) * 2 * d->width * sizeof(float));
+  // unaligned rows run in more workgroups than aligned ones
+  *bytes = round_up((size_t)norm_grad_blocks(d->rows, d->width, false) * 2 * d->width *
+                    sizeof(float));
   return FESC_OK;
 }
 

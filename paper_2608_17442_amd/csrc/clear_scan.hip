@@ -15,6 +15,7 @@
 // output itself); the state's own update does not round: the weighted inputs
 // enter as three bf16 parts that sum to the fp32 value exactly.
 #include "clear.hpp"
+#include "clear_mem.hpp"
 #include "fesc_internal.hpp"
 
 namespace fesc {
@@ -23,14 +24,6 @@ namespace {
 
 constexpr int Q = kChunk;
 constexpr int PT = kPTile;
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(8))) float f32x8;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 // A matrix operand as the 16x16 tiles take it: lane l holds row (or column)
 // l % 16 and 8 of the 32 values along the axis that is summed over, which 8
@@ -95,13 +88,6 @@ __device__ __forceinline__ f32x8 join(const f32x4& a, const f32x4& b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-template <typename T>
-__device__ __forceinline__ typename Elem<T>::Four to_four(const f32x4& v) {
-  if constexpr (sizeof(T) == 4)
-    return v;
-  else
-    return __builtin_convertvector(v, bf16x4);
-}
 __device__ __forceinline__ f32x4 widen(const bf16x4& v) { return __builtin_convertvector(v, f32x4); }
 __device__ __forceinline__ f32x4 widen(const f32x4& v) { return v; }
 
@@ -145,63 +131,6 @@ template <typename T>
 __device__ __forceinline__ float load1(const T* p) {
   return (float)*p;
 }
-
-// Global memory as the tile loads and stores see it: a uniform base and byte
-// offsets below 2^31 (clear.cpp holds strides to that).  An access at kAbsent
-// reads zero and writes nothing, so that edges need no branches, which would
-// hold back the loads behind them.
-constexpr uint32_t kAbsent = 0xfffffff0u;
-struct Mem {
-  __amdgpu_buffer_rsrc_t r;
-  __device__ __forceinline__ explicit Mem(const void* base)
-      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0x7fffffff, 0x00027000)) {}
-  __device__ __forceinline__ u32x4 load16(uint32_t at) const {
-    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
-  }
-  template <typename T>
-  __device__ __forceinline__ uint32_t load_bits(uint32_t at) const {
-    if constexpr (sizeof(T) == 4)
-      return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
-    else
-      return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
-  }
-  template <typename T>
-  __device__ __forceinline__ float load(uint32_t at) const {
-    const uint32_t w = load_bits<T>(at);
-    return __uint_as_float(sizeof(T) == 4 ? w : w << 16);
-  }
-  // Four neighbouring elements at byte offset `at`, those at or past `left`
-  // absent; whole: all or none, in one access.
-  template <typename T, bool WHOLE>
-  __device__ __forceinline__ void store_four(uint32_t at, const f32x4& v, int left) const {
-    const typename Elem<T>::Four o = to_four<T>(v);
-    if constexpr (WHOLE) {
-      if constexpr (sizeof(T) == 4)
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), r,
-                                               left > 0 ? at : kAbsent, 0, 0);
-      else
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, o), r,
-                                              left > 0 ? at : kAbsent, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t to = i < left ? at + i * (uint32_t)sizeof(T) : kAbsent;
-        if constexpr (sizeof(T) == 4)
-          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(o[i]), r, to, 0, 0);
-        else
-          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(s16x4, o)[i], r, to, 0, 0);
-      }
-    }
-  }
-  template <bool WHOLE>
-  __device__ __forceinline__ f32x4 load_four(uint32_t at, int left) const {
-    if constexpr (WHOLE) return __builtin_bit_cast(f32x4, load16(left > 0 ? at : kAbsent));
-    f32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = load<float>(i < left ? at + 4 * i : kAbsent);
-    return v;
-  }
-};
 
 // Registers of one thread for a tile of ROWS x COLS elements on its way from
 // global memory to LDS; rows and columns past the valid ones are zero.  VEC:
@@ -393,7 +322,7 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16], const T* xs, c
 // final state.  Memory bound: u and v are read once, 4 P N bytes written per
 // segment or one state per chunk.
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(256) void k_scan_states(ScanShape sh, ScanDir d0, ScanDir d1,
+__global__ __launch_bounds__(256, 2) void k_scan_states(ScanShape sh, ScanDir d0, ScanDir d1,
                                                      bool summaries) {
   constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
   __shared__ __align__(16) T xs[Q * XS];
@@ -488,7 +417,7 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
 
 // Outputs and final state.
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(256) void k_scan_out(ScanShape sh, ScanDir d, ScanOut o) {
+__global__ __launch_bounds__(256, 2) void k_scan_out(ScanShape sh, ScanDir d, ScanOut o) {
   constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
   __shared__ __align__(16) T xs[Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
@@ -742,14 +671,11 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
         cols += (m[0] + m[1]) + (m[2] + m[3]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float s = m[i];
-#pragma unroll
-          for (int x = 1; x < 16; x *= 2) s += __shfl_xor(s, x);
+          const float s = sum16(m[i]);
           if (col == 0) rowsum[tile][16 * j + 4 * g + i] = s;
         }
       }
-      cols += __shfl_xor(cols, 16);
-      cols += __shfl_xor(cols, 32);
+      cols = sum_groups(cols);
       if (g == 0) colsum[16 * tile + col] = cols;
     } else {
       const float es = ec[16 * tile + col];
@@ -767,13 +693,10 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
             widen(*reinterpret_cast<const Four*>(cs + (16 * tile + col) * NS + 16 * t + 4 * g));
         sum += (acc[0] * cv[0] + acc[1] * cv[1]) + (acc[2] * cv[2] + acc[3] * cv[3]);
       }
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
+      sum = sum_groups(sum);
       if (g == 0) us[16 * tile + col] = sum;
     }
-    float dot = rst.dot(sr, NS);
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) dot += __shfl_xor(dot, x);
+    const float dot = sum_groups(sum16(rst.dot(sr, NS)));
     if (lane == 0) dots[wave] = dot;
     __syncthreads();
     rst.store(sr, NS);
@@ -822,8 +745,7 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
             widen(*reinterpret_cast<const Four*>(bs + (16 * tile + col) * NS + 16 * t + 4 * g));
         sum += (acc[0] * bv[0] + acc[1] * bv[1]) + (acc[2] * bv[2] + acc[3] * bv[3]);
       }
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
+      sum = sum_groups(sum);
       if (g == 0) vs[16 * tile + col] = sum;
     }
     __syncthreads();

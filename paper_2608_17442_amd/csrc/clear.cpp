@@ -56,14 +56,17 @@ struct Rows {
   }
 };
 
-// Workgroups that a state pass should have: two for each of 256 compute units.
+// Workgroups that a pass over the sequence should have: two for each of 256
+// compute units.
 constexpr uint64_t kWantedGroups = 512;
 
-// A workgroup carries one head's state (a tile of 64 channels) from chunk to
-// chunk.  Where there are too few heads to fill the chip the sequence is cut
-// into segments of whole chunks, two at least (a segment's pass over its own
-// tokens is the price: x and B are read twice).
-ScanShape shape_of(const fesc_clear_scan_desc* d) {
+// A workgroup carries the states of one or two channel tiles from chunk to
+// chunk; two share what is read of B and C.  Where there are too few tiles to
+// fill the chip the sequence is cut into segments of whole chunks, two at least
+// (a segment's pass over its own tokens is the price: x and B are read twice).
+// Two tiles: where segments of four chunks fill the chip all the same.
+// `dirs`: passes that run at once.
+ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   ScanShape s{};
   s.batch = d->batch;
   s.len = d->len;
@@ -75,7 +78,10 @@ ScanShape shape_of(const fesc_clear_scan_desc* d) {
   s.la_batch = d->la_batch;
   s.chunks = (uint32_t)(((uint64_t)d->len + kChunk - 1) / kChunk);
   s.ptiles = (d->head_dim + kPTile - 1) / kPTile;
-  const uint64_t groups = (uint64_t)d->batch * d->heads * s.ptiles;
+  const uint64_t all = (uint64_t)d->batch * d->heads * s.ptiles * dirs;
+  const bool pairs = d->heads / d->groups * s.ptiles % 2 == 0;
+  s.tiles = d->dtype == FESC_BF16 && pairs && all / 2 * (s.chunks / 4) >= kWantedGroups ? 2 : 1;
+  const uint64_t groups = all / s.tiles;
   const uint64_t want = std::max<uint64_t>(1, groups ? kWantedGroups / groups : 1);
   const uint64_t segs = std::min<uint64_t>(want, std::max<uint32_t>(1, s.chunks / 2));
   s.seg_chunks = (uint32_t)((s.chunks + segs - 1) / segs);
@@ -203,7 +209,7 @@ extern "C" {
 int fesc_clear_scan_workspace(const fesc_clear_scan_desc* d, int backward, size_t* bytes) {
   if (int rc = check_scan(d)) return rc;
   if (!bytes) return fail(FESC_ERR_ARG, "null argument");
-  const ScanShape s = shape_of(d);
+  const ScanShape s = shape_of(d, backward ? 2 : 1);
   Space w(nullptr);
   ScanDir dir[2] = {};
   ScanGrad g{};
@@ -219,7 +225,7 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
                     const void* C, const float* h0, void* y, float* hT, void* workspace,
                     size_t workspace_bytes, void* stream) {
   if (int rc = check_scan(d)) return rc;
-  ScanShape s = shape_of(d);
+  ScanShape s = shape_of(d, 1);
   if (int rc = check_grid(s)) return rc;
   if (d->batch == 0) return FESC_OK;
   if (d->len == 0)
@@ -233,6 +239,7 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(h0).add(hT).add(y).len(d->head_dim)
               .len(d->d_state).ok;
+  if (!s.vec) s.tiles = 1;
   dir.u = x;
   dir.v = B;
   dir.u_token = d->x_token;
@@ -250,7 +257,7 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
                         const float* dhT, void* dx, void* dla, void* db, void* dc, float* dh0,
                         void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check_scan(d)) return rc;
-  ScanShape s = shape_of(d);
+  ScanShape s = shape_of(d, 2);
   if (int rc = check_grid(s)) return rc;
   if (d->batch == 0) return FESC_OK;
   if (d->len == 0)
@@ -267,6 +274,7 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(dy, d->dy_token, d->dy_batch).add(h0).add(dhT)
               .add(dh0).add(dx).add(db).add(dc).len(d->head_dim).len(d->d_state).ok;
+  if (!s.vec) s.tiles = 1;
   dir[0].u = x;
   dir[0].v = B;
   dir[0].u_token = d->x_token;

@@ -81,6 +81,24 @@ __device__ __forceinline__ f32x4 col_four(const float* tile, int pitch, int row0
   return f32x4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
 }
 
+// The same for the columns of state tile t: lane 4 j + i of a group takes column
+// state_col(t, j) + i.
+__device__ __forceinline__ constexpr int state_col(int t, int j) {
+  return 32 * (t / 2) + 8 * j + 4 * (t & 1);
+}
+__device__ __forceinline__ bf16x4 state_four(const __bf16* tile, int pitch, int row0, int t) {
+  const int i = threadIdx.x & 15;
+  const __bf16* p = tile + (row0 + (i >> 2)) * pitch + state_col(t, i & 3);
+  const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) s16x4*)(p));
+  return __builtin_bit_cast(bf16x4, v);
+}
+__device__ __forceinline__ f32x4 state_four(const float* tile, int pitch, int row0, int t) {
+  const int i = threadIdx.x & 15;
+  const float* p = tile + row0 * pitch + state_col(t, i >> 2) + (i & 3);
+  return f32x4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
+}
+
 __device__ __forceinline__ bf16x8 join(const bf16x4& a, const bf16x4& b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
@@ -100,13 +118,13 @@ template <>
 struct Parts<float> {
   static constexpr int kCount = 1;
   f32x8 p[1];
-  __device__ __forceinline__ Parts(const f32x4& a, const f32x4& b) { p[0] = join(a, b); }
+  __device__ __forceinline__ void split(const f32x4& a, const f32x4& b) { p[0] = join(a, b); }
 };
 template <>
 struct Parts<__bf16> {
   static constexpr int kCount = 3;
   bf16x8 p[3];
-  __device__ __forceinline__ Parts(const f32x4& a, const f32x4& b) {
+  __device__ __forceinline__ void split(const f32x4& a, const f32x4& b) {
     f32x8 v = join(a, b);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
@@ -242,9 +260,12 @@ __device__ __forceinline__ Cum cumulate(float la) {
 
 // ------------------------------------------------------------ scan kernels
 
-// One workgroup: one head's channel tile over the chunks of one segment.
-// Wave w holds the state rows p = 16 w + l % 16, entries n = 16 t + 4 g + i
-// (g = l / 16), i.e. the transpose of the state as MFMA result tiles.
+// One workgroup: HB neighbouring channel tiles (heads, where a head has one
+// tile) of one group over the chunks of one segment; what it reads of B and C
+// serves all of them.  Wave w holds, of each, the state rows p = 16 w + l % 16 as
+// the transposed MFMA result tiles t < NT / 16, entries n = state_col(t, g) + i
+// (g = l / 16): tiles 2 q and 2 q + 1 together are, in registers, the operand
+// S[p][32 q + 8 g ...] of the product with C.
 template <typename T, int NT>
 struct ScanTiles {
   static constexpr int XS = PT + Elem<T>::kPad;
@@ -252,21 +273,35 @@ struct ScanTiles {
 };
 
 struct Where {
-  uint32_t b, h, pt, seg, g;
+  uint32_t b, v, seg, g;  // v: first channel tile, among those of all heads
 };
-// Heads that read the same B and C rows lie `batch * segs` workgroups apart:
-// on one XCD where that is a multiple of 8.
+// Workgroups that read the same B and C rows lie `batch * segs` apart: on one
+// XCD where that is a multiple of 8.
+template <int HB>
 __device__ __forceinline__ Where where(const ScanShape& sh) {
   Where w;
   const uint32_t per = sh.batch * sh.segs, id = blockIdx.x;
-  const uint32_t bs = id % per, hp = id / per;
+  const uint32_t bs = id % per;
   w.b = bs / sh.segs;
   w.seg = bs % sh.segs;
-  w.h = hp / sh.ptiles;
-  w.pt = hp % sh.ptiles;
-  w.g = w.h / (sh.heads / sh.groups);
+  w.v = id / per * HB;
+  w.g = w.v / sh.ptiles / (sh.heads / sh.groups);
   return w;
 }
+
+// One channel tile of a workgroup.
+struct Head {
+  uint32_t h;     // head
+  int p0, rows;   // first channel, channels
+  uint64_t at;    // batch * heads + head
+  __device__ __forceinline__ Head(const ScanShape& sh, const Where& w, int k) {
+    const uint32_t v = w.v + k;
+    h = v / sh.ptiles;
+    p0 = v % sh.ptiles * PT;
+    rows = min(PT, (int)sh.head_dim - p0);
+    at = (uint64_t)w.b * sh.heads + h;
+  }
+};
 
 template <bool VEC, int NTILES>
 __device__ __forceinline__ void load_state(f32x4 (&s)[NTILES], const float* base, int p, int rows,
@@ -275,7 +310,7 @@ __device__ __forceinline__ void load_state(f32x4 (&s)[NTILES], const float* base
   const Mem m(base);
 #pragma unroll
   for (int t = 0; t < NTILES; ++t) {
-    const int n = 16 * t + 4 * g;
+    const int n = state_col(t, g);
     s[t] = m.load_four<VEC>((p * N + n) * 4, p < rows ? N - n : 0);
   }
 }
@@ -286,32 +321,58 @@ __device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], T* base, i
   const Mem m(base);
 #pragma unroll
   for (int t = 0; t < NTILES; ++t) {
-    const int n = 16 * t + 4 * g;
+    const int n = state_col(t, g);
     m.store_four<T, VEC>((p * N + n) * (uint32_t)sizeof(T), s[t], p < rows ? N - n : 0);
   }
 }
 
-// S' = total S + sum_r w_r x_r B_r^T over the chunk in LDS.
-template <typename T, int NT>
-__device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16], const T* xs, const T* bs,
-                                             const float* w, float total, int wave) {
-  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+// The operand with the tokens of half q of a chunk along the summed axis, from
+// a tile's columns col0 ...: tokens 32 q + 4 g + i and 32 q + 16 + 4 g + i.
+template <typename T>
+__device__ __forceinline__ typename Elem<T>::Frag token_frag(const T* tile, int pitch, int q,
+                                                             int col0) {
+  const int r = 32 * q + 4 * ((threadIdx.x & 63) >> 4);
+  return join(col_four(tile, pitch, r, col0), col_four(tile, pitch, r + 16, col0));
+}
+__device__ __forceinline__ f32x4 half(const bf16x8& v, int k) {
+  return k ? f32x4{(float)v[4], (float)v[5], (float)v[6], (float)v[7]}
+           : f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+}
+__device__ __forceinline__ f32x4 half(const f32x8& v, int k) {
+  return k ? f32x4{v[4], v[5], v[6], v[7]} : f32x4{v[0], v[1], v[2], v[3]};
+}
+
+// S' = total S + sum_r w_r x_r B_r^T over the chunk in LDS; xf: this wave's rows
+// of x as operands.
+template <typename T, int NT, int HB>
+__device__ __forceinline__ void update_state(f32x4 (&s)[HB][NT / 16],
+                                             const typename Elem<T>::Frag (&xf)[HB][2],
+                                             const T* bs, const float (*w)[Q],
+                                             const float* total) {
+  constexpr int NS = ScanTiles<T, NT>::NS;
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int t = 0; t < NT / 16; ++t) s[t] *= total;
+  for (int h = 0; h < HB; ++h) {
+    const float e = total[h];
 #pragma unroll
-  for (int k0 = 0; k0 < Q; k0 += 32) {
-    const int r0 = k0 + 8 * g;
-    const f32x4 wa = *reinterpret_cast<const f32x4*>(w + r0);
-    const f32x4 wb = *reinterpret_cast<const f32x4*>(w + r0 + 4);
-    const Parts<T> x(widen(col_four(xs, XS, r0, 16 * wave)) * wa,
-                     widen(col_four(xs, XS, r0 + 4, 16 * wave)) * wb);
+    for (int t = 0; t < NT / 16; ++t) s[h][t] *= e;
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int r = 32 * q + 4 * g;
+    Parts<T> x[HB];
+#pragma unroll
+    for (int h = 0; h < HB; ++h)
+      x[h].split(half(xf[h][q], 0) * *reinterpret_cast<const f32x4*>(w[h] + r),
+                 half(xf[h][q], 1) * *reinterpret_cast<const f32x4*>(w[h] + r + 16));
 #pragma unroll
     for (int t = 0; t < NT / 16; ++t) {
-      const typename Elem<T>::Frag b =
-          join(col_four(bs, NS, r0, 16 * t), col_four(bs, NS, r0 + 4, 16 * t));
+      const typename Elem<T>::Frag b = join(state_four(bs, NS, r, t), state_four(bs, NS, r + 16, t));
 #pragma unroll
-      for (int k = 0; k < Parts<T>::kCount; ++k) s[t] = mma(b, x.p[k], s[t]);
+      for (int k = 0; k < Parts<T>::kCount; ++k) {
+#pragma unroll
+        for (int h = 0; h < HB; ++h) s[h][t] = mma(b, x[h].p[k], s[h][t]);
+      }
     }
   }
 }
@@ -319,80 +380,107 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16], const T* xs, c
 // States only.  Segment pass (`summaries`): each segment's own state, from
 // zero, and its total decay, to seg_states and seg_decay.  Otherwise from the
 // state that enters the segment: the states that enter the chunks, and the
-// final state.  Memory bound: u and v are read once, 4 P N bytes written per
-// segment or one state per chunk.
-template <typename T, int NT, bool VEC>
+// final state.
+template <typename T, int NT, bool VEC, int HB>
 __global__ __launch_bounds__(256, 2) void k_scan_states(ScanShape sh, ScanDir d0, ScanDir d1,
-                                                     bool summaries) {
+                                                        bool summaries) {
   constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
-  __shared__ __align__(16) T xs[Q * XS];
+  __shared__ __align__(16) T xs[HB][Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
-  __shared__ __align__(16) float wt[Q];
-  __shared__ float total;
+  __shared__ __align__(16) float wt[HB][Q];
+  __shared__ float total[HB];
   const ScanDir& d = blockIdx.z ? d1 : d0;
-  const Where at = where(sh);
+  const Where at = where<HB>(sh);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int P = sh.head_dim, N = sh.d_state;
-  const int p0 = at.pt * PT, rows = min(PT, P - p0), p = 16 * wave + (lane & 15);
+  const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + (lane & 15);
   // segments and chunks are counted in the direction of the pass
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
   if (summaries && at.seg + 1 == sh.segs) return;  // no segment follows the last
-  const uint64_t head = (uint64_t)at.b * sh.heads + at.h;
   const uint64_t size = (uint64_t)P * N;
-  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + p0;
+  const T* u = (const T*)d.u + at.b * d.u_batch;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch;
 
-  f32x4 s[NT / 16];
-  const float* from = summaries       ? nullptr
-                      : d.seg_states ? d.seg_states + (head * sh.segs + at.seg) * size
-                      : d.init       ? d.init + head * size
-                                     : nullptr;
-  if (from) {
-    load_state<VEC>(s, from + (uint64_t)p0 * N, p, rows, N);
-  } else {
+  f32x4 s[HB][NT / 16];
 #pragma unroll
-    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
+  for (int h = 0; h < HB; ++h) {
+    const Head hd(sh, at, h);
+    const float* from = summaries      ? nullptr
+                        : d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
+                        : d.init       ? d.init + hd.at * size
+                                       : nullptr;
+    if (from) {
+      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N);
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT / 16; ++t) s[h][t] = f32x4{0, 0, 0, 0};
+    }
   }
-  Stage<T, Q, PT, 256, VEC> xst;
+  Stage<T, Q, PT, 256, VEC> xst[HB];
   Stage<T, Q, NT, 256, VEC> bst;
-  float lav = 0.0f;
+  float lav = 0.0f;  // wave h < HB: log decay of token `lane` of tile h
+  const uint32_t la_at = (lane * (uint32_t)sh.la_token + Head(sh, at, wave < HB ? wave : 0).h) *
+                         (uint32_t)sizeof(T);
   auto fetch = [&](int k) {
     const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
     const int64_t t0 = (int64_t)c * Q;
     const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    lav = Mem(la + t0 * sh.la_token)
-              .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
-    xst.load(u + t0 * d.u_token, d.u_token, n, rows);
+    if (wave < HB)
+      lav = Mem(la + t0 * sh.la_token)
+                .load<T>(lane < n ? la_at : kAbsent);
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      const Head hd(sh, at, h);
+      xst[h].load(u + t0 * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+    }
     bst.load(v + t0 * d.v_token, d.v_token, n, N);
   };
   fetch(0);
-  float decay = 1.0f;
+  float decay[HB];
+#pragma unroll
+  for (int h = 0; h < HB; ++h) decay[h] = 1.0f;
   for (int k = 0; k < count; ++k) {
     if (d.chunk_states && !summaries) {
       const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
-      store_state<VEC>(s, (T*)d.chunk_states + (head * sh.chunks + c) * size + (uint64_t)p0 * N, p, rows, N);
+#pragma unroll
+      for (int h = 0; h < HB; ++h) {
+        const Head hd(sh, at, h);
+        store_state<VEC>(s[h], (T*)d.chunk_states + (hd.at * sh.chunks + c) * size +
+                                   (uint64_t)hd.p0 * N, p, hd.rows, N);
+      }
     }
     Cum cum;
-    if (wave == 0) cum = cumulate(lav);
+    if (wave < HB) cum = cumulate(lav);
     __syncthreads();
-    xst.store(xs, XS);
+#pragma unroll
+    for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
     bst.store(bs, NS);
-    if (wave == 0) {
-      wt[lane] = d.reverse ? cum.e : cum.w;
-      if (lane == 0) total = cum.total;
+    if (wave < HB) {
+      wt[wave][lane] = d.reverse ? cum.e : cum.w;
+      if (lane == 0) total[wave] = cum.total;
     }
     __syncthreads();
     if (k + 1 < count) fetch(k + 1);
-    update_state<T, NT>(s, xs, bs, wt, total, wave);
-    decay *= total;
+    typename Elem<T>::Frag xf[HB][2];
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[h], XS, q, 16 * wave);
+      decay[h] *= total[h];
+    }
+    update_state<T, NT, HB>(s, xf, bs, wt, total);
   }
-  if (summaries) {
-    store_state<VEC>(s, d.seg_states + (head * sh.segs + at.seg + 1) * size + (uint64_t)p0 * N, p, rows, N);
-    if (threadIdx.x == 0 && at.pt == 0) d.seg_decay[head * sh.segs + at.seg] = decay;
-  } else if (d.fin && at.seg + 1 == sh.segs) {
-    store_state<VEC>(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N);
+#pragma unroll
+  for (int h = 0; h < HB; ++h) {
+    const Head hd(sh, at, h);
+    if (summaries) {
+      store_state<VEC>(s[h], d.seg_states + (hd.at * sh.segs + at.seg + 1) * size +
+                                 (uint64_t)hd.p0 * N, p, hd.rows, N);
+      if (threadIdx.x == 0 && hd.p0 == 0) d.seg_decay[hd.at * sh.segs + at.seg] = decay[h];
+    } else if (d.fin && at.seg + 1 == sh.segs) {
+      store_state<VEC>(s[h], d.fin + hd.at * size + (uint64_t)hd.p0 * N, p, hd.rows, N);
+    }
   }
 }
 
@@ -415,128 +503,167 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
   }
 }
 
-// Outputs and final state.
-template <typename T, int NT, bool VEC>
+// Outputs and final state.  Per chunk: G = C B^T once for the HB tiles, its
+// product with each tile's decays to LDS (wave w the tokens of 16-token tile w),
+// then wave w forms y^T for its 16 channels and all tokens from that, x and its
+// own part of the state, which never leaves its registers, and updates the
+// state.
+template <typename T, int NT, bool VEC, int HB>
 __global__ __launch_bounds__(256, 2) void k_scan_out(ScanShape sh, ScanDir d, ScanOut o) {
   constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
-  __shared__ __align__(16) T xs[Q * XS];
+  constexpr int NQ = NT / 32;
+  __shared__ __align__(16) T xs[HB][Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
-  __shared__ __align__(16) T ss[PT * NS];
-  __shared__ __align__(16) float hi[Q], lo[Q], ec[Q], wt[Q];
-  __shared__ float total;
+  __shared__ __align__(16) T lg[HB][Q * XS];
+  __shared__ __align__(16) float hi[HB][Q], lo[HB][Q], ec[HB][Q], wt[HB][Q];
+  __shared__ float total[HB];
   using Frag = typename Elem<T>::Frag;
-  using Four = typename Elem<T>::Four;
-  const Where at = where(sh);
+  const Where at = where<HB>(sh);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const int P = sh.head_dim, N = sh.d_state;
-  const int p0 = at.pt * PT, rows = min(PT, P - p0), p = 16 * wave + col;
+  const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + col;
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
-  const uint64_t head = (uint64_t)at.b * sh.heads + at.h;
   const uint64_t size = (uint64_t)P * N;
-  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + p0;
+  const T* u = (const T*)d.u + at.b * d.u_batch;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
   const T* cc = (const T*)o.c + at.b * o.c_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
-  T* y = (T*)o.y + ((uint64_t)at.b * sh.len * sh.heads + at.h) * P + p0;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch;
 
-  f32x4 s[NT / 16];
-  const float* from = d.seg_states ? d.seg_states + (head * sh.segs + at.seg) * size
-                      : d.init     ? d.init + head * size
-                                   : nullptr;
-  if (from) {
-    load_state<VEC>(s, from + (uint64_t)p0 * N, p, rows, N);
-  } else {
+  f32x4 s[HB][NT / 16];
 #pragma unroll
-    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
+  for (int h = 0; h < HB; ++h) {
+    const Head hd(sh, at, h);
+    const float* from = d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
+                        : d.init     ? d.init + hd.at * size
+                                     : nullptr;
+    if (from) {
+      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N);
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT / 16; ++t) s[h][t] = f32x4{0, 0, 0, 0};
+    }
   }
-  Stage<T, Q, PT, 256, VEC> xst;
+  Stage<T, Q, PT, 256, VEC> xst[HB];
   Stage<T, Q, NT, 256, VEC> bst, cst;
-  float lav = 0.0f;
+  float lav = 0.0f;  // wave h < HB: log decay of token `lane` of tile h
+  const uint32_t la_at = (lane * (uint32_t)sh.la_token + Head(sh, at, wave < HB ? wave : 0).h) *
+                         (uint32_t)sizeof(T);
   auto fetch = [&](int k) {
     const int64_t t0 = (int64_t)(first + k) * Q;
     const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    lav = Mem(la + t0 * sh.la_token)
-              .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
-    xst.load(u + t0 * d.u_token, d.u_token, n, rows);
+    if (wave < HB)
+      lav = Mem(la + t0 * sh.la_token)
+                .load<T>(lane < n ? la_at : kAbsent);
     bst.load(v + t0 * d.v_token, d.v_token, n, N);
     cst.load(cc + t0 * o.c_token, o.c_token, n, N);
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      const Head hd(sh, at, h);
+      xst[h].load(u + t0 * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+    }
   };
   fetch(0);
   for (int k = 0; k < count; ++k) {
     Cum cum;
-    if (wave == 0) cum = cumulate(lav);
+    if (wave < HB) cum = cumulate(lav);
     __syncthreads();
-    xst.store(xs, XS);
     bst.store(bs, NS);
     cst.store(cs, NS);
 #pragma unroll
-    for (int t = 0; t < NT / 16; ++t)
-      *reinterpret_cast<Four*>(ss + p * NS + 16 * t + 4 * g) = to_four<T>(s[t]);
-    if (wave == 0) {
-      hi[lane] = cum.hi;
-      lo[lane] = cum.lo;
-      ec[lane] = cum.e;
-      wt[lane] = cum.w;
-      if (lane == 0) total = cum.total;
+    for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
+    if (wave < HB) {
+      hi[wave][lane] = cum.hi;
+      lo[wave][lane] = cum.lo;
+      ec[wave][lane] = cum.e;
+      wt[wave][lane] = cum.w;
+      if (lane == 0) total[wave] = cum.total;
     }
     __syncthreads();
     if (k + 1 < count) fetch(k + 1);
-
-    // Tokens s = 16 wave + col.  Tiles of (C B^T)^T have rows r and columns s:
-    // a lane's four values are the operand of the product with x that sums
-    // over r, so they never leave the registers.
-    Frag cf[NT / 32];
+    {
+      // rows r = 16 j + 4 g + i, column s = 16 wave + col
+      Frag cf[NQ];
 #pragma unroll
-    for (int q = 0; q < NT / 32; ++q) cf[q] = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
-    const float hs = hi[16 * wave + col], ls = lo[16 * wave + col];
-    Four w[4];
+      for (int q = 0; q < NQ; ++q)
+        cf[q] = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
+      f32x4 gt[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        gt[j] = f32x4{0, 0, 0, 0};
+        if (j <= wave) {
+#pragma unroll
+          for (int q = 0; q < NQ; ++q)
+            gt[j] = mma(row_frag(bs + (16 * j + col) * NS + 32 * q + 8 * g), cf[q], gt[j]);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < HB; ++h) {
+        const float hs = hi[h][16 * wave + col], ls = lo[h][16 * wave + col];
+        f32x4 w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j] = f32x4{0, 0, 0, 0};
+          if (j <= wave) {
+            const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[h] + 16 * j + 4 * g);
+            const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[h] + 16 * j + 4 * g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const bool seen = j < wave || 4 * g + i <= col;
+              w[j][i] = seen ? gt[j][i] * exp2_diff(hs, ls, hr[i], lr[i]) : 0.0f;
+            }
+          }
+        }
+        // position 32 q + 8 g + 4 e + i holds token 32 q + 16 e + 4 g + i, so that
+        // a row read gives the operand that matches token_frag
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          *reinterpret_cast<Frag*>(lg[h] + (16 * wave + col) * XS + 32 * q + 8 * g) =
+              join(to_four<T>(w[2 * q]), to_four<T>(w[2 * q + 1]));
+      }
+    }
+    __syncthreads();
+    Frag xf[HB][2], sf[HB][NQ];
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[h], XS, q, 16 * wave);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+        sf[h][q] = join(to_four<T>(s[h][2 * q]), to_four<T>(s[h][2 * q + 1]));
+    }
+    const int64_t t0 = (int64_t)(first + k) * Q;
+    // y^T: rows p = 16 wave + 4 g + i, column s = 16 j + col
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      f32x4 acc = {0, 0, 0, 0};
-      if (j <= wave) {
+      Frag cf[NQ];
 #pragma unroll
-        for (int q = 0; q < NT / 32; ++q)
-          acc = mma(row_frag(bs + (16 * j + col) * NS + 32 * q + 8 * g), cf[q], acc);
-        const f32x4 hr = *reinterpret_cast<const f32x4*>(hi + 16 * j + 4 * g);
-        const f32x4 lr = *reinterpret_cast<const f32x4*>(lo + 16 * j + 4 * g);
+      for (int q = 0; q < NQ; ++q) cf[q] = row_frag(cs + (16 * j + col) * NS + 32 * q + 8 * g);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool seen = j < wave || 4 * g + i <= col;
-          acc[i] = seen ? acc[i] * exp2_diff(hs, ls, hr[i], lr[i]) : 0.0f;
-        }
+      for (int h = 0; h < HB; ++h) {
+        const Head hd(sh, at, h);
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) acc = mma(sf[h][q], cf[q], acc);
+        acc *= ec[h][16 * j + col];
+#pragma unroll
+        for (int q = 0; q <= j / 2; ++q)
+          acc = mma(xf[h][q], row_frag(lg[h] + (16 * j + col) * XS + 32 * q + 8 * g), acc);
+        const Mem ym((T*)o.y + (((uint64_t)at.b * sh.len + t0) * sh.heads + hd.h) * P + hd.p0);
+        const int pp = 16 * wave + 4 * g;
+        ym.store_four<T, VEC>(((16 * j + col) * sh.heads * P + pp) * (uint32_t)sizeof(T), acc,
+                              t0 + 16 * j + col < (int64_t)sh.len ? hd.rows - pp : 0);
       }
-      w[j] = to_four<T>(acc);
     }
-    // y^T: rows p = 16 t + 4 g + i, column s
-    const float es = ec[16 * wave + col];
-    const int64_t t0 = (int64_t)(first + k) * Q;
-    const Mem ym(y + t0 * sh.heads * P);
-    const uint32_t yat = (16 * wave + col) * sh.heads * P * (uint32_t)sizeof(T);
-    const bool here = t0 + 16 * wave + col < (int64_t)sh.len;
-#pragma unroll
-    for (int t = 0; t < PT / 16; ++t) {
-      f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-      for (int q = 0; q < NT / 32; ++q)
-        acc = mma(row_frag(ss + (16 * t + col) * NS + 32 * q + 8 * g), cf[q], acc);
-      acc *= es;
-#pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        if (j <= wave) {
-          const Frag xf = join(col_four(xs, XS, 16 * j + 4 * g, 16 * t),
-                               col_four(xs, XS, 16 * j + 16 + 4 * g, 16 * t));
-          acc = mma(xf, join(w[j], w[j + 1]), acc);
-        }
-      }
-      const int pp = 16 * t + 4 * g;
-      ym.store_four<T, VEC>(yat + pp * (uint32_t)sizeof(T), acc, here ? rows - pp : 0);
-    }
-    update_state<T, NT>(s, xs, bs, wt, total, wave);
+    update_state<T, NT, HB>(s, xf, bs, wt, total);
   }
-  if (d.fin && at.seg + 1 == sh.segs)
-    store_state<VEC>(s, d.fin + head * size + (uint64_t)p0 * N, p, rows, N);
+  if (d.fin && at.seg + 1 == sh.segs) {
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      const Head hd(sh, at, h);
+      store_state<VEC>(s[h], d.fin + hd.at * size + (uint64_t)hd.p0 * N, p, hd.rows, N);
+    }
+  }
 }
 
 // ------------------------------------------------------------ gradient
@@ -878,19 +1005,38 @@ __global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to
   if (i < count) to[i] = from ? from[i] : 0.0f;
 }
 
-template <typename T, int NT, bool VEC>
+template <typename T, int NT, bool VEC, int HB>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
   const ScanDir &d0 = d[0], &d1 = d[nd - 1];
-  const dim3 grid(sh.batch * sh.segs * sh.heads * sh.ptiles, 1, nd);
+  const dim3 grid(sh.batch * sh.segs * (sh.heads * sh.ptiles / HB), 1, nd);
   if (sh.segs > 1) {
-    k_scan_states<T, NT, VEC><<<grid, 256, 0, s>>>(sh, d0, d1, true);
+    k_scan_states<T, NT, VEC, HB><<<grid, 256, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
     const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
     k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
     if (hipError_t e = hipGetLastError()) return e;
   }
   if (!main) return hipSuccess;
-  k_scan_states<T, NT, VEC><<<grid, 256, 0, s>>>(sh, d0, d1, false);
+  k_scan_states<T, NT, VEC, HB><<<grid, 256, 0, s>>>(sh, d0, d1, false);
+  return hipGetLastError();
+}
+template <typename T, int NT, bool VEC>
+hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && VEC)
+    if (sh.tiles == 2) return states<T, NT, VEC, 2>(sh, d, nd, main, s);
+  return states<T, NT, VEC, 1>(sh, d, nd, main, s);
+}
+template <typename T, int NT, bool VEC>
+hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
+  if (hipError_t e = states<T, NT, VEC>(sh, &d, 1, false, s)) return e;
+  const uint32_t grid = sh.batch * sh.segs * (sh.heads * sh.ptiles / sh.tiles);
+  if constexpr (sizeof(T) == 2 && VEC) {
+    if (sh.tiles == 2) {
+      k_scan_out<T, NT, VEC, 2><<<grid, 256, 0, s>>>(sh, d, o);
+      return hipGetLastError();
+    }
+  }
+  k_scan_out<T, NT, VEC, 1><<<grid, 256, 0, s>>>(sh, d, o);
   return hipGetLastError();
 }
 
@@ -912,11 +1058,7 @@ hipError_t launch_scan_states(uint32_t dtype, const ScanShape& sh, const ScanDir
 
 hipError_t launch_scan_out(uint32_t dtype, const ScanShape& sh, const ScanDir& d,
                            const ScanOut& o, hipStream_t s) {
-#define CALL(T, NT, VEC) states<T, NT, VEC>(sh, &d, 1, false, s)
-  if (hipError_t e = FESC_SCAN_CASES(dtype, sh, CALL)) return e;
-#undef CALL
-  const uint32_t grid = sh.batch * sh.segs * sh.heads * sh.ptiles;
-#define CALL(T, NT, VEC) (k_scan_out<T, NT, VEC><<<grid, 256, 0, s>>>(sh, d, o), hipGetLastError())
+#define CALL(T, NT, VEC) outputs<T, NT, VEC>(sh, d, o, s)
   return FESC_SCAN_CASES(dtype, sh, CALL);
 #undef CALL
 }

@@ -229,6 +229,15 @@ struct Cum {
 __device__ __forceinline__ float exp2_diff(float hs, float ls, float hr, float lr) {
   return __builtin_amdgcn_exp2f((hs - hr) + (ls - lr));
 }
+// The same where `seen`, else 0 (without a branch around the exponential).
+__device__ __forceinline__ float exp2_seen(bool seen, float hs, float ls, float hr, float lr) {
+  const float d = (hs - hr) + (ls - lr);
+  return __builtin_amdgcn_exp2f(seen ? d : -INFINITY);
+}
+// The wave's number, known to be the same for all its lanes.
+__device__ __forceinline__ int wave_id() {
+  return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+}
 // One step of the scan over a wave: adds the value that the DPP control moves
 // here (0 where it moves none).
 template <int CTRL, int ROWS>
@@ -391,7 +400,7 @@ __global__ __launch_bounds__(256, 2) void k_scan_states(ScanShape sh, ScanDir d0
   __shared__ float total[HB];
   const ScanDir& d = blockIdx.z ? d1 : d0;
   const Where at = where<HB>(sh);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = wave_id(), lane = threadIdx.x & 63;
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + (lane & 15);
   // segments and chunks are counted in the direction of the pass
   const int first = at.seg * sh.seg_chunks;
@@ -520,7 +529,7 @@ __global__ __launch_bounds__(256, 2) void k_scan_out(ScanShape sh, ScanDir d, Sc
   __shared__ float total[HB];
   using Frag = typename Elem<T>::Frag;
   const Where at = where<HB>(sh);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + col;
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
@@ -610,7 +619,7 @@ __global__ __launch_bounds__(256, 2) void k_scan_out(ScanShape sh, ScanDir d, Sc
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const bool seen = j < wave || 4 * g + i <= col;
-              w[j][i] = seen ? gt[j][i] * exp2_diff(hs, ls, hr[i], lr[i]) : 0.0f;
+              w[j][i] = gt[j][i] * exp2_seen(seen, hs, ls, hr[i], lr[i]);
             }
           }
         }
@@ -692,7 +701,7 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   __shared__ float us[Q], vs[Q], colsum[Q], rowsum[4][Q], dots[8];
   using Frag = typename Elem<T>::Frag;
   using Four = typename Elem<T>::Four;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   const bool left = wave < 4;  // waves of dx
   const int tile = wave & 3;
   const int P = sh.head_dim, N = sh.d_state;
@@ -786,9 +795,8 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
           const f32x4 ls = *reinterpret_cast<const f32x4*>(lo + 16 * j + 4 * g);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const bool seen = j > tile || 4 * g + i >= col;
-            e[i] = seen ? exp2_diff(hs[i], ls[i], hr, lr) : 0.0f;
-            m[i] = seen ? m[i] * e[i] : 0.0f;
+            e[i] = exp2_seen(j > tile || 4 * g + i >= col, hs[i], ls[i], hr, lr);
+            m[i] *= e[i];
           }
           wk[j] += m;
           e *= gt[j];

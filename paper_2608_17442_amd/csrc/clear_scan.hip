@@ -270,11 +270,11 @@ __device__ __forceinline__ Cum cumulate(float la) {
 // ------------------------------------------------------------ scan kernels
 
 // One workgroup: HB neighbouring channel tiles (heads, where a head has one
-// tile) of one group over the chunks of one segment; what it reads of B and C
-// serves all of them.  Wave w holds, of each, the state rows p = 16 w + l % 16 as
-// the transposed MFMA result tiles t < NT / 16, entries n = state_col(t, g) + i
-// (g = l / 16): tiles 2 q and 2 q + 1 together are, in registers, the operand
-// S[p][32 q + 8 g ...] of the product with C.
+// tile) of one group over the chunks of one segment; what it stages of B and C
+// serves all of them.  Wave 4 h + w holds, of tile h, the state rows
+// p = 16 w + l % 16 as the transposed MFMA result tiles t < NT / 16, entries
+// n = state_col(t, g) + i (g = l / 16): tiles 2 q and 2 q + 1 together are, in
+// registers, the operand S[p][32 q + 8 g ...] of the product with C.
 template <typename T, int NT>
 struct ScanTiles {
   static constexpr int XS = PT + Elem<T>::kPad;
@@ -353,35 +353,25 @@ __device__ __forceinline__ f32x4 half(const f32x8& v, int k) {
 
 // S' = total S + sum_r w_r x_r B_r^T over the chunk in LDS; xf: this wave's rows
 // of x as operands.
-template <typename T, int NT, int HB>
-__device__ __forceinline__ void update_state(f32x4 (&s)[HB][NT / 16],
-                                             const typename Elem<T>::Frag (&xf)[HB][2],
-                                             const T* bs, const float (*w)[Q],
-                                             const float* total) {
+template <typename T, int NT>
+__device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16],
+                                             const typename Elem<T>::Frag (&xf)[2], const T* bs,
+                                             const float* w, float total) {
   constexpr int NS = ScanTiles<T, NT>::NS;
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int h = 0; h < HB; ++h) {
-    const float e = total[h];
-#pragma unroll
-    for (int t = 0; t < NT / 16; ++t) s[h][t] *= e;
-  }
+  for (int t = 0; t < NT / 16; ++t) s[t] *= total;
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int r = 32 * q + 4 * g;
-    Parts<T> x[HB];
-#pragma unroll
-    for (int h = 0; h < HB; ++h)
-      x[h].split(half(xf[h][q], 0) * *reinterpret_cast<const f32x4*>(w[h] + r),
-                 half(xf[h][q], 1) * *reinterpret_cast<const f32x4*>(w[h] + r + 16));
+    Parts<T> x;
+    x.split(half(xf[q], 0) * *reinterpret_cast<const f32x4*>(w + r),
+            half(xf[q], 1) * *reinterpret_cast<const f32x4*>(w + r + 16));
 #pragma unroll
     for (int t = 0; t < NT / 16; ++t) {
       const typename Elem<T>::Frag b = join(state_four(bs, NS, r, t), state_four(bs, NS, r + 16, t));
 #pragma unroll
-      for (int k = 0; k < Parts<T>::kCount; ++k) {
-#pragma unroll
-        for (int h = 0; h < HB; ++h) s[h][t] = mma(b, x[h].p[k], s[h][t]);
-      }
+      for (int k = 0; k < Parts<T>::kCount; ++k) s[t] = mma(b, x.p[k], s[t]);
     }
   }
 }
@@ -391,105 +381,86 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[HB][NT / 16],
 // state that enters the segment: the states that enter the chunks, and the
 // final state.
 template <typename T, int NT, bool VEC, int HB>
-__global__ __launch_bounds__(256, 2) void k_scan_states(ScanShape sh, ScanDir d0, ScanDir d1,
-                                                        bool summaries) {
-  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+__global__ __launch_bounds__(256 * HB, 2 * HB) void k_scan_states(ScanShape sh, ScanDir d0,
+                                                                  ScanDir d1, bool summaries) {
+  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS, TH = 256 * HB;
   __shared__ __align__(16) T xs[HB][Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) float wt[HB][Q];
   __shared__ float total[HB];
   const ScanDir& d = blockIdx.z ? d1 : d0;
   const Where at = where<HB>(sh);
-  const int wave = wave_id(), lane = threadIdx.x & 63;
+  const int wave = wave_id() & 3, mine = wave_id() >> 2, lane = threadIdx.x & 63;
+  const Head hd(sh, at, mine);
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + (lane & 15);
   // segments and chunks are counted in the direction of the pass
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
   if (summaries && at.seg + 1 == sh.segs) return;  // no segment follows the last
-  const uint64_t size = (uint64_t)P * N;
+  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)hd.p0 * N;
   const T* u = (const T*)d.u + at.b * d.u_batch;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + hd.h;
 
-  f32x4 s[HB][NT / 16];
+  f32x4 s[NT / 16];
+  const float* from = summaries      ? nullptr
+                      : d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
+                      : d.init       ? d.init + hd.at * size
+                                     : nullptr;
+  if (from) {
+    load_state<VEC>(s, from + tile, p, hd.rows, N);
+  } else {
 #pragma unroll
-  for (int h = 0; h < HB; ++h) {
-    const Head hd(sh, at, h);
-    const float* from = summaries      ? nullptr
-                        : d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
-                        : d.init       ? d.init + hd.at * size
-                                       : nullptr;
-    if (from) {
-      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N);
-    } else {
-#pragma unroll
-      for (int t = 0; t < NT / 16; ++t) s[h][t] = f32x4{0, 0, 0, 0};
-    }
+    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
   }
-  Stage<T, Q, PT, 256, VEC> xst[HB];
-  Stage<T, Q, NT, 256, VEC> bst;
-  float lav = 0.0f;  // wave h < HB: log decay of token `lane` of tile h
-  const uint32_t la_at = (lane * (uint32_t)sh.la_token + Head(sh, at, wave < HB ? wave : 0).h) *
-                         (uint32_t)sizeof(T);
+  Stage<T, Q, PT, TH, VEC> xst[HB];
+  Stage<T, Q, NT, TH, VEC> bst;
+  float lav = 0.0f;  // log decay of token `lane`
   auto fetch = [&](int k) {
     const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
     const int64_t t0 = (int64_t)c * Q;
     const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    if (wave < HB)
+    if (wave == 0)
       lav = Mem(la + t0 * sh.la_token)
-                .load<T>(lane < n ? la_at : kAbsent);
+                .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
-      const Head hd(sh, at, h);
-      xst[h].load(u + t0 * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+      const Head hh(sh, at, h);
+      xst[h].load(u + t0 * d.u_token + (int64_t)hh.h * P + hh.p0, d.u_token, n, hh.rows);
     }
     bst.load(v + t0 * d.v_token, d.v_token, n, N);
   };
   fetch(0);
-  float decay[HB];
-#pragma unroll
-  for (int h = 0; h < HB; ++h) decay[h] = 1.0f;
+  float decay = 1.0f;
   for (int k = 0; k < count; ++k) {
     if (d.chunk_states && !summaries) {
       const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
-#pragma unroll
-      for (int h = 0; h < HB; ++h) {
-        const Head hd(sh, at, h);
-        store_state<VEC>(s[h], (T*)d.chunk_states + (hd.at * sh.chunks + c) * size +
-                                   (uint64_t)hd.p0 * N, p, hd.rows, N);
-      }
+      store_state<VEC>(s, (T*)d.chunk_states + (hd.at * sh.chunks + c) * size + tile, p, hd.rows,
+                       N);
     }
     Cum cum;
-    if (wave < HB) cum = cumulate(lav);
+    if (wave == 0) cum = cumulate(lav);
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
     bst.store(bs, NS);
-    if (wave < HB) {
-      wt[wave][lane] = d.reverse ? cum.e : cum.w;
-      if (lane == 0) total[wave] = cum.total;
+    if (wave == 0) {
+      wt[mine][lane] = d.reverse ? cum.e : cum.w;
+      if (lane == 0) total[mine] = cum.total;
     }
     __syncthreads();
     if (k + 1 < count) fetch(k + 1);
-    typename Elem<T>::Frag xf[HB][2];
+    typename Elem<T>::Frag xf[2];
 #pragma unroll
-    for (int h = 0; h < HB; ++h) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[h], XS, q, 16 * wave);
-      decay[h] *= total[h];
-    }
-    update_state<T, NT, HB>(s, xf, bs, wt, total);
+    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs[mine], XS, q, 16 * wave);
+    decay *= total[mine];
+    update_state<T, NT>(s, xf, bs, wt[mine], total[mine]);
   }
-#pragma unroll
-  for (int h = 0; h < HB; ++h) {
-    const Head hd(sh, at, h);
-    if (summaries) {
-      store_state<VEC>(s[h], d.seg_states + (hd.at * sh.segs + at.seg + 1) * size +
-                                 (uint64_t)hd.p0 * N, p, hd.rows, N);
-      if (threadIdx.x == 0 && hd.p0 == 0) d.seg_decay[hd.at * sh.segs + at.seg] = decay[h];
-    } else if (d.fin && at.seg + 1 == sh.segs) {
-      store_state<VEC>(s[h], d.fin + hd.at * size + (uint64_t)hd.p0 * N, p, hd.rows, N);
-    }
+  if (summaries) {
+    store_state<VEC>(s, d.seg_states + (hd.at * sh.segs + at.seg + 1) * size + tile, p, hd.rows, N);
+    if (wave == 0 && lane == 0 && hd.p0 == 0) d.seg_decay[hd.at * sh.segs + at.seg] = decay;
+  } else if (d.fin && at.seg + 1 == sh.segs) {
+    store_state<VEC>(s, d.fin + hd.at * size + tile, p, hd.rows, N);
   }
 }
 
@@ -512,14 +483,15 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
   }
 }
 
-// Outputs and final state.  Per chunk: G = C B^T once for the HB tiles, its
-// product with each tile's decays to LDS (wave w the tokens of 16-token tile w),
-// then wave w forms y^T for its 16 channels and all tokens from that, x and its
-// own part of the state, which never leaves its registers, and updates the
-// state.
+// Outputs and final state.  Per chunk: G = C B^T once for the HB tiles (wave
+// 4 e + w: token tile w, the tokens r of half e, or of both where HB = 1), its
+// product with each tile's decays to LDS; then wave 4 h + w forms y^T for its 16
+// channels and all tokens from that, x and its own part of the state, which
+// never leaves its registers, and updates the state.
 template <typename T, int NT, bool VEC, int HB>
-__global__ __launch_bounds__(256, 2) void k_scan_out(ScanShape sh, ScanDir d, ScanOut o) {
-  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+__global__ __launch_bounds__(256 * HB, 2 * HB) void k_scan_out(ScanShape sh, ScanDir d,
+                                                               ScanOut o) {
+  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS, TH = 256 * HB;
   constexpr int NQ = NT / 32;
   __shared__ __align__(16) T xs[HB][Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
@@ -529,150 +501,129 @@ __global__ __launch_bounds__(256, 2) void k_scan_out(ScanShape sh, ScanDir d, Sc
   __shared__ float total[HB];
   using Frag = typename Elem<T>::Frag;
   const Where at = where<HB>(sh);
-  const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const int wave = wave_id() & 3, mine = wave_id() >> 2;
+  const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const Head hd(sh, at, mine);
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + col;
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
-  const uint64_t size = (uint64_t)P * N;
+  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)hd.p0 * N;
   const T* u = (const T*)d.u + at.b * d.u_batch;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
   const T* cc = (const T*)o.c + at.b * o.c_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + hd.h;
 
-  f32x4 s[HB][NT / 16];
+  f32x4 s[NT / 16];
+  const float* from = d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
+                      : d.init     ? d.init + hd.at * size
+                                   : nullptr;
+  if (from) {
+    load_state<VEC>(s, from + tile, p, hd.rows, N);
+  } else {
 #pragma unroll
-  for (int h = 0; h < HB; ++h) {
-    const Head hd(sh, at, h);
-    const float* from = d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
-                        : d.init     ? d.init + hd.at * size
-                                     : nullptr;
-    if (from) {
-      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N);
-    } else {
-#pragma unroll
-      for (int t = 0; t < NT / 16; ++t) s[h][t] = f32x4{0, 0, 0, 0};
-    }
+    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
   }
-  Stage<T, Q, PT, 256, VEC> xst[HB];
-  Stage<T, Q, NT, 256, VEC> bst, cst;
-  float lav = 0.0f;  // wave h < HB: log decay of token `lane` of tile h
-  const uint32_t la_at = (lane * (uint32_t)sh.la_token + Head(sh, at, wave < HB ? wave : 0).h) *
-                         (uint32_t)sizeof(T);
+  Stage<T, Q, PT, TH, VEC> xst[HB];
+  Stage<T, Q, NT, TH, VEC> bst, cst;
+  float lav = 0.0f;  // log decay of token `lane`
   auto fetch = [&](int k) {
     const int64_t t0 = (int64_t)(first + k) * Q;
     const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    if (wave < HB)
+    if (wave == 0)
       lav = Mem(la + t0 * sh.la_token)
-                .load<T>(lane < n ? la_at : kAbsent);
+                .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
     bst.load(v + t0 * d.v_token, d.v_token, n, N);
     cst.load(cc + t0 * o.c_token, o.c_token, n, N);
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
-      const Head hd(sh, at, h);
-      xst[h].load(u + t0 * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+      const Head hh(sh, at, h);
+      xst[h].load(u + t0 * d.u_token + (int64_t)hh.h * P + hh.p0, d.u_token, n, hh.rows);
     }
   };
   fetch(0);
   for (int k = 0; k < count; ++k) {
     Cum cum;
-    if (wave < HB) cum = cumulate(lav);
+    if (wave == 0) cum = cumulate(lav);
     __syncthreads();
     bst.store(bs, NS);
     cst.store(cs, NS);
 #pragma unroll
     for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
-    if (wave < HB) {
-      hi[wave][lane] = cum.hi;
-      lo[wave][lane] = cum.lo;
-      ec[wave][lane] = cum.e;
-      wt[wave][lane] = cum.w;
-      if (lane == 0) total[wave] = cum.total;
+    if (wave == 0) {
+      hi[mine][lane] = cum.hi;
+      lo[mine][lane] = cum.lo;
+      ec[mine][lane] = cum.e;
+      wt[mine][lane] = cum.w;
+      if (lane == 0) total[mine] = cum.total;
     }
     __syncthreads();
     if (k + 1 < count) fetch(k + 1);
-    {
+    if (HB == 1 || 2 * mine <= wave) {
       // rows r = 16 j + 4 g + i, column s = 16 wave + col
       Frag cf[NQ];
 #pragma unroll
       for (int q = 0; q < NQ; ++q)
         cf[q] = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
-      f32x4 gt[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        gt[j] = f32x4{0, 0, 0, 0};
-        if (j <= wave) {
+      for (int e = 0; e < 2 / HB; ++e) {
+        const int half_of = HB == 1 ? e : mine;  // tokens r of this half
+        if (2 * half_of > wave) break;
+        f32x4 gt[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const int j = 2 * half_of + f;
+          gt[f] = f32x4{0, 0, 0, 0};
 #pragma unroll
           for (int q = 0; q < NQ; ++q)
-            gt[j] = mma(row_frag(bs + (16 * j + col) * NS + 32 * q + 8 * g), cf[q], gt[j]);
+            gt[f] = mma(row_frag(bs + (16 * j + col) * NS + 32 * q + 8 * g), cf[q], gt[f]);
         }
-      }
 #pragma unroll
-      for (int h = 0; h < HB; ++h) {
-        const float hs = hi[h][16 * wave + col], ls = lo[h][16 * wave + col];
-        f32x4 w[4];
+        for (int h = 0; h < HB; ++h) {
+          const float hs = hi[h][16 * wave + col], ls = lo[h][16 * wave + col];
+          f32x4 w[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[j] = f32x4{0, 0, 0, 0};
-          if (j <= wave) {
-            const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[h] + 16 * j + 4 * g);
-            const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[h] + 16 * j + 4 * g);
+          for (int f = 0; f < 2; ++f) {
+            const int r = 32 * half_of + 16 * f + 4 * g;
+            const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[h] + r);
+            const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[h] + r);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const bool seen = j < wave || 4 * g + i <= col;
-              w[j][i] = gt[j][i] * exp2_seen(seen, hs, ls, hr[i], lr[i]);
-            }
+            for (int i = 0; i < 4; ++i)
+              w[f][i] = gt[f][i] * exp2_seen(r + i <= 16 * wave + col, hs, ls, hr[i], lr[i]);
           }
+          // position 32 q + 8 g + 4 f + i holds token 32 q + 16 f + 4 g + i, so that
+          // a row read gives the operand that matches token_frag
+          *reinterpret_cast<Frag*>(lg[h] + (16 * wave + col) * XS + 32 * half_of + 8 * g) =
+              join(to_four<T>(w[0]), to_four<T>(w[1]));
         }
-        // position 32 q + 8 g + 4 e + i holds token 32 q + 16 e + 4 g + i, so that
-        // a row read gives the operand that matches token_frag
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-          *reinterpret_cast<Frag*>(lg[h] + (16 * wave + col) * XS + 32 * q + 8 * g) =
-              join(to_four<T>(w[2 * q]), to_four<T>(w[2 * q + 1]));
       }
     }
     __syncthreads();
-    Frag xf[HB][2], sf[HB][NQ];
+    Frag xf[2], sf[NQ];
 #pragma unroll
-    for (int h = 0; h < HB; ++h) {
+    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs[mine], XS, q, 16 * wave);
 #pragma unroll
-      for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[h], XS, q, 16 * wave);
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-        sf[h][q] = join(to_four<T>(s[h][2 * q]), to_four<T>(s[h][2 * q + 1]));
-    }
+    for (int q = 0; q < NQ; ++q) sf[q] = join(to_four<T>(s[2 * q]), to_four<T>(s[2 * q + 1]));
     const int64_t t0 = (int64_t)(first + k) * Q;
+    const Mem ym((T*)o.y + (((uint64_t)at.b * sh.len + t0) * sh.heads + hd.h) * P + hd.p0);
+    const int pp = 16 * wave + 4 * g;
     // y^T: rows p = 16 wave + 4 g + i, column s = 16 j + col
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      Frag cf[NQ];
+      f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) cf[q] = row_frag(cs + (16 * j + col) * NS + 32 * q + 8 * g);
+      for (int q = 0; q < NQ; ++q)
+        acc = mma(sf[q], row_frag(cs + (16 * j + col) * NS + 32 * q + 8 * g), acc);
+      acc *= ec[mine][16 * j + col];
 #pragma unroll
-      for (int h = 0; h < HB; ++h) {
-        const Head hd(sh, at, h);
-        f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) acc = mma(sf[h][q], cf[q], acc);
-        acc *= ec[h][16 * j + col];
-#pragma unroll
-        for (int q = 0; q <= j / 2; ++q)
-          acc = mma(xf[h][q], row_frag(lg[h] + (16 * j + col) * XS + 32 * q + 8 * g), acc);
-        const Mem ym((T*)o.y + (((uint64_t)at.b * sh.len + t0) * sh.heads + hd.h) * P + hd.p0);
-        const int pp = 16 * wave + 4 * g;
-        ym.store_four<T, VEC>(((16 * j + col) * sh.heads * P + pp) * (uint32_t)sizeof(T), acc,
-                              t0 + 16 * j + col < (int64_t)sh.len ? hd.rows - pp : 0);
-      }
+      for (int q = 0; q <= j / 2; ++q)
+        acc = mma(xf[q], row_frag(lg[mine] + (16 * j + col) * XS + 32 * q + 8 * g), acc);
+      ym.store_four<T, VEC>(((16 * j + col) * sh.heads * P + pp) * (uint32_t)sizeof(T), acc,
+                            t0 + 16 * j + col < (int64_t)sh.len ? hd.rows - pp : 0);
     }
-    update_state<T, NT, HB>(s, xf, bs, wt, total);
+    update_state<T, NT>(s, xf, bs, wt[mine], total[mine]);
   }
-  if (d.fin && at.seg + 1 == sh.segs) {
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const Head hd(sh, at, h);
-      store_state<VEC>(s[h], d.fin + hd.at * size + (uint64_t)hd.p0 * N, p, hd.rows, N);
-    }
-  }
+  if (d.fin && at.seg + 1 == sh.segs)
+    store_state<VEC>(s, d.fin + hd.at * size + tile, p, hd.rows, N);
 }
 
 // ------------------------------------------------------------ gradient
@@ -1018,14 +969,14 @@ hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipS
   const ScanDir &d0 = d[0], &d1 = d[nd - 1];
   const dim3 grid(sh.batch * sh.segs * (sh.heads * sh.ptiles / HB), 1, nd);
   if (sh.segs > 1) {
-    k_scan_states<T, NT, VEC, HB><<<grid, 256, 0, s>>>(sh, d0, d1, true);
+    k_scan_states<T, NT, VEC, HB><<<grid, 256 * HB, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
     const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
     k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
     if (hipError_t e = hipGetLastError()) return e;
   }
   if (!main) return hipSuccess;
-  k_scan_states<T, NT, VEC, HB><<<grid, 256, 0, s>>>(sh, d0, d1, false);
+  k_scan_states<T, NT, VEC, HB><<<grid, 256 * HB, 0, s>>>(sh, d0, d1, false);
   return hipGetLastError();
 }
 template <typename T, int NT, bool VEC>
@@ -1040,7 +991,7 @@ hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipS
   const uint32_t grid = sh.batch * sh.segs * (sh.heads * sh.ptiles / sh.tiles);
   if constexpr (sizeof(T) == 2 && VEC) {
     if (sh.tiles == 2) {
-      k_scan_out<T, NT, VEC, 2><<<grid, 256, 0, s>>>(sh, d, o);
+      k_scan_out<T, NT, VEC, 2><<<grid, 512, 0, s>>>(sh, d, o);
       return hipGetLastError();
     }
   }

@@ -56,16 +56,14 @@ struct Rows {
   }
 };
 
-// Workgroups that a pass over the sequence should have: two for each of 256
-// compute units.
-constexpr uint64_t kWantedGroups = 512;
+// Workgroups that a pass over the sequence should have: enough to occupy most
+// of the 256 compute units.
+constexpr uint64_t kWantedGroups = 192;
 
-// A workgroup carries the states of one or two channel tiles from chunk to
-// chunk; two share what is read of B and C.  Where there are too few tiles to
-// fill the chip the sequence is cut into segments of whole chunks, two at least
-// (a segment's pass over its own tokens is the price: x and B are read twice).
-// Two tiles: where segments of four chunks fill the chip all the same.
-// `dirs`: passes that run at once.
+// A workgroup carries the state of one channel tile from chunk to chunk.
+// Where there are too few tiles to fill the chip the sequence is cut into
+// segments of whole chunks, two at least (a segment's pass over its own tokens
+// is the price: x and B are read twice).  `dirs`: passes that run at once.
 ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   ScanShape s{};
   s.batch = d->batch;
@@ -78,10 +76,7 @@ ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   s.la_batch = d->la_batch;
   s.chunks = (uint32_t)(((uint64_t)d->len + kChunk - 1) / kChunk);
   s.ptiles = (d->head_dim + kPTile - 1) / kPTile;
-  const uint64_t all = (uint64_t)d->batch * d->heads * s.ptiles * dirs;
-  const bool pairs = d->heads / d->groups * s.ptiles % 2 == 0;
-  s.tiles = d->dtype == FESC_BF16 && pairs && all / 2 * (s.chunks / 4) >= kWantedGroups ? 2 : 1;
-  const uint64_t groups = all / s.tiles;
+  const uint64_t groups = (uint64_t)d->batch * d->heads * s.ptiles * dirs;
   const uint64_t want = std::max<uint64_t>(1, groups ? kWantedGroups / groups : 1);
   const uint64_t segs = std::min<uint64_t>(want, std::max<uint32_t>(1, s.chunks / 2));
   s.seg_chunks = (uint32_t)((s.chunks + segs - 1) / segs);
@@ -138,7 +133,7 @@ void grad_space(Space& w, const ScanShape& s, uint32_t dtype, ScanDir* dir, Scan
 int check_grid(const ScanShape& s) {
   const uint64_t bh = (uint64_t)s.batch * s.heads;
   const uint64_t join = ((uint64_t)s.head_dim * s.d_state + 255) / 256;
-  if (bh * s.ptiles * s.segs >= kMaxGrid256 || bh * join >= kMaxGrid256 ||
+  if (bh * s.ptiles * s.segs >= kMaxGrid512 || bh * join >= kMaxGrid256 ||
       (uint64_t)s.batch * s.chunks >= kMaxGrid512 ||
       (uint64_t)s.batch * s.len * s.groups * s.d_state >= kMaxGrid256 * 256)
     return fail(FESC_ERR_ARG, "batch * len * heads too large for one call");
@@ -239,7 +234,6 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(h0).add(hT).add(y).len(d->head_dim)
               .len(d->d_state).ok;
-  if (!s.vec) s.tiles = 1;
   dir.u = x;
   dir.v = B;
   dir.u_token = d->x_token;
@@ -274,7 +268,6 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(dy, d->dy_token, d->dy_batch).add(h0).add(dhT)
               .add(dh0).add(dx).add(db).add(dc).len(d->head_dim).len(d->d_state).ok;
-  if (!s.vec) s.tiles = 1;
   dir[0].u = x;
   dir[0].v = B;
   dir[0].u_token = d->x_token;

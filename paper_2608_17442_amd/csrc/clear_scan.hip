@@ -192,6 +192,31 @@ struct Stage {
       *reinterpret_cast<u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit) = r[k];
     }
   }
+  __device__ __forceinline__ void take(const T* tile, int pitch) {
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      r[k] = *reinterpret_cast<const u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit);
+    }
+  }
+  __device__ __forceinline__ void put(T* base, uint32_t pitch, int rows, int cols) const {
+    const Mem m(base);
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int i = threadIdx.x + k * THREADS;
+      const int row = i / kPerRow, col = i % kPerRow * kUnit;
+      const uint32_t at = (row * pitch + col) * (uint32_t)sizeof(T);
+      if constexpr (VEC) {
+        m.store16(row < rows && col < cols ? at : kAbsent, r[k]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j)
+          m.store_bits<T>(row < rows && col + j < cols ? at + j * (uint32_t)sizeof(T) : kAbsent,
+                          sizeof(T) == 4 ? r[k][j * sizeof(T) / 4]
+                                         : r[k][j * sizeof(T) / 4] >> (16 * (j & 1)) & 0xffffu);
+      }
+    }
+  }
   // sum of the products of these values with those at the same places of a tile
   __device__ __forceinline__ float dot(const T* tile, int pitch) const {
     float s = 0.0f;
@@ -269,68 +294,59 @@ __device__ __forceinline__ Cum cumulate(float la) {
 
 // ------------------------------------------------------------ scan kernels
 
-// One workgroup: HB neighbouring channel tiles (heads, where a head has one
-// tile) of one group over the chunks of one segment; what it stages of B and C
-// serves all of them.  Wave 4 h + w holds, of tile h, the state rows
-// p = 16 w + l % 16 as the transposed MFMA result tiles t < NT / 16, entries
-// n = state_col(t, g) + i (g = l / 16): tiles 2 q and 2 q + 1 together are, in
-// registers, the operand S[p][32 q + 8 g ...] of the product with C.
+// One workgroup: one channel tile of a head over the chunks of one segment.
+// Wave 4 e + w holds the state rows p = 16 w + l % 16, of them the entries n of
+// half e, as transposed MFMA result tiles t = e NT / 32 ... (e + 1) NT / 32 - 1
+// with n = state_col(t, g) + i (g = l / 16): tiles 2 q and 2 q + 1 together are, in
+// registers, the operand S[p][32 q + 8 g ...] of the product with C.  Eight
+// waves per head: what bounds these kernels is the time from chunk to chunk,
+// which halves with the work of each wave.
+constexpr int kScanThreads = 512;
 template <typename T, int NT>
 struct ScanTiles {
   static constexpr int XS = PT + Elem<T>::kPad;
   static constexpr int NS = NT + Elem<T>::kPad;
+  static constexpr int kOwn = NT / 32;  // state tiles of a wave
 };
 
+// Heads that read the same B and C rows lie `batch * segs` workgroups apart:
+// on one XCD where that is a multiple of 8.
 struct Where {
-  uint32_t b, v, seg, g;  // v: first channel tile, among those of all heads
-};
-// Workgroups that read the same B and C rows lie `batch * segs` apart: on one
-// XCD where that is a multiple of 8.
-template <int HB>
-__device__ __forceinline__ Where where(const ScanShape& sh) {
-  Where w;
-  const uint32_t per = sh.batch * sh.segs, id = blockIdx.x;
-  const uint32_t bs = id % per;
-  w.b = bs / sh.segs;
-  w.seg = bs % sh.segs;
-  w.v = id / per * HB;
-  w.g = w.v / sh.ptiles / (sh.heads / sh.groups);
-  return w;
-}
-
-// One channel tile of a workgroup.
-struct Head {
-  uint32_t h;     // head
-  int p0, rows;   // first channel, channels
-  uint64_t at;    // batch * heads + head
-  __device__ __forceinline__ Head(const ScanShape& sh, const Where& w, int k) {
-    const uint32_t v = w.v + k;
+  uint32_t b, h, seg, g;
+  int p0, rows;  // first channel of the tile, its channels
+  uint64_t at;   // batch * heads + head
+  __device__ __forceinline__ explicit Where(const ScanShape& sh) {
+    const uint32_t per = sh.batch * sh.segs, bs = blockIdx.x % per, v = blockIdx.x / per;
+    b = bs / sh.segs;
+    seg = bs % sh.segs;
     h = v / sh.ptiles;
+    g = h / (sh.heads / sh.groups);
     p0 = v % sh.ptiles * PT;
     rows = min(PT, (int)sh.head_dim - p0);
-    at = (uint64_t)w.b * sh.heads + h;
+    at = (uint64_t)b * sh.heads + h;
   }
 };
 
+// Tiles t0 ... of the state from and to memory.
 template <bool VEC, int NTILES>
 __device__ __forceinline__ void load_state(f32x4 (&s)[NTILES], const float* base, int p, int rows,
-                                           int N) {
+                                           int N, int t0) {
   const int g = (threadIdx.x & 63) >> 4;
   const Mem m(base);
 #pragma unroll
   for (int t = 0; t < NTILES; ++t) {
-    const int n = state_col(t, g);
+    const int n = state_col(t0 + t, g);
     s[t] = m.load_four<VEC>((p * N + n) * 4, p < rows ? N - n : 0);
   }
 }
 template <bool VEC, typename T, int NTILES>
 __device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], T* base, int p, int rows,
-                                            int N) {
+                                            int N, int t0) {
   const int g = (threadIdx.x & 63) >> 4;
   const Mem m(base);
 #pragma unroll
   for (int t = 0; t < NTILES; ++t) {
-    const int n = state_col(t, g);
+    const int n = state_col(t0 + t, g);
     m.store_four<T, VEC>((p * N + n) * (uint32_t)sizeof(T), s[t], p < rows ? N - n : 0);
   }
 }
@@ -352,15 +368,16 @@ __device__ __forceinline__ f32x4 half(const f32x8& v, int k) {
 }
 
 // S' = total S + sum_r w_r x_r B_r^T over the chunk in LDS; xf: this wave's rows
-// of x as operands.
+// of x as operands.  Two tiles at a time, whose products do not wait for each
+// other's sums.
 template <typename T, int NT>
-__device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16],
+__device__ __forceinline__ void update_state(f32x4 (&s)[NT / 32],
                                              const typename Elem<T>::Frag (&xf)[2], const T* bs,
-                                             const float* w, float total) {
+                                             const float* w, float total, int t0) {
   constexpr int NS = ScanTiles<T, NT>::NS;
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int t = 0; t < NT / 16; ++t) s[t] *= total;
+  for (int t = 0; t < NT / 32; ++t) s[t] *= total;
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int r = 32 * q + 4 * g;
@@ -368,10 +385,16 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16],
     x.split(half(xf[q], 0) * *reinterpret_cast<const f32x4*>(w + r),
             half(xf[q], 1) * *reinterpret_cast<const f32x4*>(w + r + 16));
 #pragma unroll
-    for (int t = 0; t < NT / 16; ++t) {
-      const typename Elem<T>::Frag b = join(state_four(bs, NS, r, t), state_four(bs, NS, r + 16, t));
+    for (int t = 0; t < NT / 32; t += 2) {
+      typename Elem<T>::Frag b[2];
 #pragma unroll
-      for (int k = 0; k < Parts<T>::kCount; ++k) s[t] = mma(b, x.p[k], s[t]);
+      for (int f = 0; f < 2; ++f)
+        b[f] = join(state_four(bs, NS, r, t0 + t + f), state_four(bs, NS, r + 16, t0 + t + f));
+#pragma unroll
+      for (int k = 0; k < Parts<T>::kCount; ++k) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f) s[t + f] = mma(b[f], x.p[k], s[t + f]);
+      }
     }
   }
 }
@@ -379,88 +402,84 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[NT / 16],
 // States only.  Segment pass (`summaries`): each segment's own state, from
 // zero, and its total decay, to seg_states and seg_decay.  Otherwise from the
 // state that enters the segment: the states that enter the chunks, and the
-// final state.
-template <typename T, int NT, bool VEC, int HB>
-__global__ __launch_bounds__(256 * HB, 2 * HB) void k_scan_states(ScanShape sh, ScanDir d0,
-                                                                  ScanDir d1, bool summaries) {
-  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS, TH = 256 * HB;
-  __shared__ __align__(16) T xs[HB][Q * XS];
-  __shared__ __align__(16) T bs[Q * NS];
-  __shared__ __align__(16) float wt[HB][Q];
-  __shared__ float total[HB];
+// final state.  Chunks lie in LDS in turn in two places: one barrier each.
+template <typename T, int NT, bool VEC>
+__global__ __launch_bounds__(kScanThreads, 2) void k_scan_states(ScanShape sh, ScanDir d0,
+                                                                 ScanDir d1, bool summaries) {
+  using Tiles = ScanTiles<T, NT>;
+  constexpr int XS = Tiles::XS, NS = Tiles::NS;
+  __shared__ __align__(16) T xs[2][Q * XS];
+  __shared__ __align__(16) T bs[2][Q * NS];
+  __shared__ __align__(16) float wt[2][Q];
+  __shared__ float total[2];
   const ScanDir& d = blockIdx.z ? d1 : d0;
-  const Where at = where<HB>(sh);
-  const int wave = wave_id() & 3, mine = wave_id() >> 2, lane = threadIdx.x & 63;
-  const Head hd(sh, at, mine);
+  const Where at(sh);
+  const int wave = wave_id() & 3, t0 = (wave_id() >> 2) * Tiles::kOwn, lane = threadIdx.x & 63;
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + (lane & 15);
   // segments and chunks are counted in the direction of the pass
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
   if (summaries && at.seg + 1 == sh.segs) return;  // no segment follows the last
-  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)hd.p0 * N;
-  const T* u = (const T*)d.u + at.b * d.u_batch;
+  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)at.p0 * N;
+  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + at.p0;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch + hd.h;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
 
-  f32x4 s[NT / 16];
+  f32x4 s[Tiles::kOwn];
   const float* from = summaries      ? nullptr
-                      : d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
-                      : d.init       ? d.init + hd.at * size
+                      : d.seg_states ? d.seg_states + (at.at * sh.segs + at.seg) * size
+                      : d.init       ? d.init + at.at * size
                                      : nullptr;
   if (from) {
-    load_state<VEC>(s, from + tile, p, hd.rows, N);
+    load_state<VEC>(s, from + tile, p, at.rows, N, t0);
   } else {
 #pragma unroll
-    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
+    for (int t = 0; t < Tiles::kOwn; ++t) s[t] = f32x4{0, 0, 0, 0};
   }
-  Stage<T, Q, PT, TH, VEC> xst[HB];
-  Stage<T, Q, NT, TH, VEC> bst;
-  float lav = 0.0f;  // log decay of token `lane`
+  Stage<T, Q, PT, kScanThreads, VEC> xst;
+  Stage<T, Q, NT, kScanThreads, VEC> bst;
+  float lav = 0.0f;  // wave 0: log decay of token `lane`
+  auto chunk = [&](int k) { return d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k; };
   auto fetch = [&](int k) {
-    const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
-    const int64_t t0 = (int64_t)c * Q;
-    const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    if (wave == 0)
-      lav = Mem(la + t0 * sh.la_token)
+    const int64_t from = (int64_t)chunk(k) * Q;
+    const int n = min((int64_t)Q, (int64_t)sh.len - from);
+    if (wave_id() == 0)
+      lav = Mem(la + from * sh.la_token)
                 .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const Head hh(sh, at, h);
-      xst[h].load(u + t0 * d.u_token + (int64_t)hh.h * P + hh.p0, d.u_token, n, hh.rows);
+    xst.load(u + from * d.u_token, d.u_token, n, at.rows);
+    bst.load(v + from * d.v_token, d.v_token, n, N);
+  };
+  auto place = [&](int k) {
+    xst.store(xs[k & 1], XS);
+    bst.store(bs[k & 1], NS);
+    if (wave_id() == 0) {
+      const Cum cum = cumulate(lav);
+      wt[k & 1][lane] = d.reverse ? cum.e : cum.w;
+      if (lane == 0) total[k & 1] = cum.total;
     }
-    bst.load(v + t0 * d.v_token, d.v_token, n, N);
+    __syncthreads();
   };
   fetch(0);
+  place(0);
   float decay = 1.0f;
   for (int k = 0; k < count; ++k) {
-    if (d.chunk_states && !summaries) {
-      const int c = d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k;
-      store_state<VEC>(s, (T*)d.chunk_states + (hd.at * sh.chunks + c) * size + tile, p, hd.rows,
-                       N);
-    }
-    Cum cum;
-    if (wave == 0) cum = cumulate(lav);
-    __syncthreads();
-#pragma unroll
-    for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
-    bst.store(bs, NS);
-    if (wave == 0) {
-      wt[mine][lane] = d.reverse ? cum.e : cum.w;
-      if (lane == 0) total[mine] = cum.total;
-    }
-    __syncthreads();
     if (k + 1 < count) fetch(k + 1);
+    if (d.chunk_states && !summaries)
+      store_state<VEC>(s, (T*)d.chunk_states + (at.at * sh.chunks + chunk(k)) * size + tile, p,
+                       at.rows, N, t0);
     typename Elem<T>::Frag xf[2];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs[mine], XS, q, 16 * wave);
-    decay *= total[mine];
-    update_state<T, NT>(s, xf, bs, wt[mine], total[mine]);
+    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs[k & 1], XS, q, 16 * wave);
+    decay *= total[k & 1];
+    update_state<T, NT>(s, xf, bs[k & 1], wt[k & 1], total[k & 1], t0);
+    if (k + 1 < count) place(k + 1);
   }
   if (summaries) {
-    store_state<VEC>(s, d.seg_states + (hd.at * sh.segs + at.seg + 1) * size + tile, p, hd.rows, N);
-    if (wave == 0 && lane == 0 && hd.p0 == 0) d.seg_decay[hd.at * sh.segs + at.seg] = decay;
+    store_state<VEC>(s, d.seg_states + (at.at * sh.segs + at.seg + 1) * size + tile, p, at.rows, N,
+                     t0);
+    if (threadIdx.x == 0 && at.p0 == 0) d.seg_decay[at.at * sh.segs + at.seg] = decay;
   } else if (d.fin && at.seg + 1 == sh.segs) {
-    store_state<VEC>(s, d.fin + hd.at * size + tile, p, hd.rows, N);
+    store_state<VEC>(s, d.fin + at.at * size + tile, p, at.rows, N, t0);
   }
 }
 
@@ -483,147 +502,171 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
   }
 }
 
-// Outputs and final state.  Per chunk: G = C B^T once for the HB tiles (wave
-// 4 e + w: token tile w, the tokens r of half e, or of both where HB = 1), its
-// product with each tile's decays to LDS; then wave 4 h + w forms y^T for its 16
-// channels and all tokens from that, x and its own part of the state, which
-// never leaves its registers, and updates the state.
-template <typename T, int NT, bool VEC, int HB>
-__global__ __launch_bounds__(256 * HB, 2 * HB) void k_scan_out(ScanShape sh, ScanDir d,
-                                                               ScanOut o) {
-  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS, TH = 256 * HB;
-  constexpr int NQ = NT / 32;
-  __shared__ __align__(16) T xs[HB][Q * XS];
+// Outputs and final state.  Per chunk: wave 4 e + w forms the columns of token
+// tile w of G^T, G = C B^T, for the tokens r of half e, and writes their product
+// with the decays to LDS; then y^T for its 16 channels and the tokens of half e
+// from that, x and the state (its own half of it from the registers, the other
+// through LDS), and updates its part of the state.
+template <typename T, int NT, bool VEC>
+__global__ __launch_bounds__(kScanThreads, sizeof(T) == 2 ? 4 : 2) void k_scan_out(ScanShape sh,
+                                                                                   ScanDir d,
+                                                                                   ScanOut o) {
+  using Tiles = ScanTiles<T, NT>;
+  constexpr int XS = Tiles::XS, NS = Tiles::NS;
+  constexpr int NQ = NT / 32, HQ = NT / 64;  // operands of the state, and of half of it
+  __shared__ __align__(16) T xs[Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
-  __shared__ __align__(16) T lg[HB][Q * XS];
-  __shared__ __align__(16) float hi[HB][Q], lo[HB][Q], ec[HB][Q], wt[HB][Q];
-  __shared__ float total[HB];
+  __shared__ __align__(16) T lg[Q * XS];
+  __shared__ __align__(16) T ys[Q * XS];
+  __shared__ __align__(16) T ss[NQ][PT * 32];  // the state's operands, lane by lane
+  __shared__ __align__(16) float hi[2][Q], lo[2][Q], ec[2][Q], wt[2][Q];
+  __shared__ float total[2];
   using Frag = typename Elem<T>::Frag;
-  const Where at = where<HB>(sh);
-  const int wave = wave_id() & 3, mine = wave_id() >> 2;
+  const Where at(sh);
+  const int id = wave_id(), wave = id & 3, e = id >> 2, t0 = e * Tiles::kOwn;
   const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const Head hd(sh, at, mine);
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + col;
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
-  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)hd.p0 * N;
-  const T* u = (const T*)d.u + at.b * d.u_batch;
+  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)at.p0 * N;
+  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + at.p0;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
   const T* cc = (const T*)o.c + at.b * o.c_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch + hd.h;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
+  T* y = (T*)o.y + ((uint64_t)at.b * sh.len * sh.heads + at.h) * P + at.p0;
 
-  f32x4 s[NT / 16];
-  const float* from = d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
-                      : d.init     ? d.init + hd.at * size
+  f32x4 s[Tiles::kOwn];
+  const float* from = d.seg_states ? d.seg_states + (at.at * sh.segs + at.seg) * size
+                      : d.init     ? d.init + at.at * size
                                    : nullptr;
   if (from) {
-    load_state<VEC>(s, from + tile, p, hd.rows, N);
+    load_state<VEC>(s, from + tile, p, at.rows, N, t0);
   } else {
 #pragma unroll
-    for (int t = 0; t < NT / 16; ++t) s[t] = f32x4{0, 0, 0, 0};
+    for (int t = 0; t < Tiles::kOwn; ++t) s[t] = f32x4{0, 0, 0, 0};
   }
-  Stage<T, Q, PT, TH, VEC> xst[HB];
-  Stage<T, Q, NT, TH, VEC> bst, cst;
-  float lav = 0.0f;  // log decay of token `lane`
+  Stage<T, Q, PT, kScanThreads, VEC> xst, yst;
+  Stage<T, Q, NT, kScanThreads, VEC> bst, cst;
+  auto start = [&](int k) { return (int64_t)(first + k) * Q; };
+  auto tokens = [&](int k) { return (int)min((int64_t)Q, (int64_t)sh.len - start(k)); };
   auto fetch = [&](int k) {
-    const int64_t t0 = (int64_t)(first + k) * Q;
-    const int n = min((int64_t)Q, (int64_t)sh.len - t0);
-    if (wave == 0)
-      lav = Mem(la + t0 * sh.la_token)
-                .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
-    bst.load(v + t0 * d.v_token, d.v_token, n, N);
-    cst.load(cc + t0 * o.c_token, o.c_token, n, N);
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const Head hh(sh, at, h);
-      xst[h].load(u + t0 * d.u_token + (int64_t)hh.h * P + hh.p0, d.u_token, n, hh.rows);
-    }
+    const int n = tokens(k);
+    bst.load(v + start(k) * d.v_token, d.v_token, n, N);
+    cst.load(cc + start(k) * o.c_token, o.c_token, n, N);
+    xst.load(u + start(k) * d.u_token, d.u_token, n, at.rows);
+  };
+  // Running sums of chunk k, by the wave that has least of G: two chunks ahead
+  // from memory, one ahead into LDS.
+  constexpr int kSums = 4;
+  float lav = 0.0f;  // log decay of token `lane`
+  auto fetch_la = [&](int k) {
+    if (k < count)
+      lav = Mem(la + start(k) * sh.la_token)
+                .load<T>(lane < tokens(k) ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T)
+                                          : kAbsent);
+  };
+  auto sums = [&](int k) {
+    const Cum cum = cumulate(lav);
+    hi[k & 1][lane] = cum.hi;
+    lo[k & 1][lane] = cum.lo;
+    ec[k & 1][lane] = cum.e;
+    wt[k & 1][lane] = cum.w;
+    if (lane == 0) total[k & 1] = cum.total;
   };
   fetch(0);
+  if (id == kSums) {
+    fetch_la(0);
+    sums(0);
+    fetch_la(1);
+  }
+  // Two barriers a chunk.  Between the first and the second the tiles of the
+  // chunk, the state's operands and the outputs of the chunk before are read and
+  // lg is written; after the second lg is read and the tiles, operands and
+  // outputs are written.
   for (int k = 0; k < count; ++k) {
-    Cum cum;
-    if (wave == 0) cum = cumulate(lav);
-    __syncthreads();
+    const int now = k & 1;
     bst.store(bs, NS);
     cst.store(cs, NS);
+    xst.store(xs, XS);
+    Frag sf[NQ];
 #pragma unroll
-    for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
-    if (wave == 0) {
-      hi[mine][lane] = cum.hi;
-      lo[mine][lane] = cum.lo;
-      ec[mine][lane] = cum.e;
-      wt[mine][lane] = cum.w;
-      if (lane == 0) total[mine] = cum.total;
+    for (int q = 0; q < HQ; ++q) {
+      const Frag f = join(to_four<T>(s[2 * q]), to_four<T>(s[2 * q + 1]));
+      *reinterpret_cast<Frag*>(ss[e * HQ + q] + (64 * wave + lane) * 8) = f;
     }
     __syncthreads();
     if (k + 1 < count) fetch(k + 1);
-    if (HB == 1 || 2 * mine <= wave) {
-      // rows r = 16 j + 4 g + i, column s = 16 wave + col
-      Frag cf[NQ];
+    if (k) {
+      yst.take(ys, XS);
+      yst.put(y + start(k - 1) * sh.heads * P, sh.heads * P, tokens(k - 1), at.rows);
+    }
+    if (id == kSums && k + 1 < count) {
+      sums(k + 1);
+      fetch_la(k + 2);
+    }
+    if (2 * e <= wave) {
+      // rows r = 32 e + 16 f + 4 g + i, column s = 16 wave + col
+      f32x4 gt[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-      for (int q = 0; q < NQ; ++q)
-        cf[q] = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
+      for (int q = 0; q < NQ; ++q) {
+        const Frag cf = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
 #pragma unroll
-      for (int e = 0; e < 2 / HB; ++e) {
-        const int half_of = HB == 1 ? e : mine;  // tokens r of this half
-        if (2 * half_of > wave) break;
-        f32x4 gt[2];
+        for (int f = 0; f < 2; ++f)
+          gt[f] = mma(row_frag(bs + (32 * e + 16 * f + col) * NS + 32 * q + 8 * g), cf, gt[f]);
+      }
+      const float hs = hi[now][16 * wave + col], ls = lo[now][16 * wave + col];
+      f32x4 w[2];
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          const int j = 2 * half_of + f;
-          gt[f] = f32x4{0, 0, 0, 0};
+      for (int f = 0; f < 2; ++f) {
+        const int r = 32 * e + 16 * f + 4 * g;
+        const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[now] + r);
+        const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[now] + r);
 #pragma unroll
-          for (int q = 0; q < NQ; ++q)
-            gt[f] = mma(row_frag(bs + (16 * j + col) * NS + 32 * q + 8 * g), cf[q], gt[f]);
-        }
+        for (int i = 0; i < 4; ++i)
+          w[f][i] = gt[f][i] * exp2_seen(r + i <= 16 * wave + col, hs, ls, hr[i], lr[i]);
+      }
+      // position 32 q + 8 g + 4 f + i holds token 32 q + 16 f + 4 g + i, so that a
+      // row read gives the operand that matches token_frag
+      *reinterpret_cast<Frag*>(lg + (16 * wave + col) * XS + 32 * e + 8 * g) =
+          join(to_four<T>(w[0]), to_four<T>(w[1]));
+    }
+    Frag xf[2];
 #pragma unroll
-        for (int h = 0; h < HB; ++h) {
-          const float hs = hi[h][16 * wave + col], ls = lo[h][16 * wave + col];
-          f32x4 w[2];
+    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs, XS, q, 16 * wave);
 #pragma unroll
-          for (int f = 0; f < 2; ++f) {
-            const int r = 32 * half_of + 16 * f + 4 * g;
-            const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[h] + r);
-            const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[h] + r);
+    for (int q = 0; q < NQ; ++q)
+      sf[q] = *reinterpret_cast<const Frag*>(ss[q] + (64 * wave + lane) * 8);
+    // y^T: rows p = 16 wave + 4 g + i, columns s = 32 e + 16 j + col
+    f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[f][i] = gt[f][i] * exp2_seen(r + i <= 16 * wave + col, hs, ls, hr[i], lr[i]);
-          }
-          // position 32 q + 8 g + 4 f + i holds token 32 q + 16 f + 4 g + i, so that
-          // a row read gives the operand that matches token_frag
-          *reinterpret_cast<Frag*>(lg[h] + (16 * wave + col) * XS + 32 * half_of + 8 * g) =
-              join(to_four<T>(w[0]), to_four<T>(w[1]));
-        }
+    for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        acc[j] = mma(sf[q], row_frag(cs + (32 * e + 16 * j + col) * NS + 32 * q + 8 * g), acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[j] *= ec[now][32 * e + 16 * j + col];
+    update_state<T, NT>(s, xf, bs, wt[now], total[now], t0);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (q <= e) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          acc[j] = mma(xf[q], row_frag(lg + (32 * e + 16 * j + col) * XS + 32 * q + 8 * g), acc[j]);
       }
     }
-    __syncthreads();
-    Frag xf[2], sf[NQ];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs[mine], XS, q, 16 * wave);
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) sf[q] = join(to_four<T>(s[2 * q]), to_four<T>(s[2 * q + 1]));
-    const int64_t t0 = (int64_t)(first + k) * Q;
-    const Mem ym((T*)o.y + (((uint64_t)at.b * sh.len + t0) * sh.heads + hd.h) * P + hd.p0);
-    const int pp = 16 * wave + 4 * g;
-    // y^T: rows p = 16 wave + 4 g + i, column s = 16 j + col
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-        acc = mma(sf[q], row_frag(cs + (16 * j + col) * NS + 32 * q + 8 * g), acc);
-      acc *= ec[mine][16 * j + col];
-#pragma unroll
-      for (int q = 0; q <= j / 2; ++q)
-        acc = mma(xf[q], row_frag(lg[mine] + (16 * j + col) * XS + 32 * q + 8 * g), acc);
-      ym.store_four<T, VEC>(((16 * j + col) * sh.heads * P + pp) * (uint32_t)sizeof(T), acc,
-                            t0 + 16 * j + col < (int64_t)sh.len ? hd.rows - pp : 0);
-    }
-    update_state<T, NT>(s, xf, bs, wt[mine], total[mine]);
+    for (int j = 0; j < 2; ++j)
+      *reinterpret_cast<typename Elem<T>::Four*>(ys + (32 * e + 16 * j + col) * XS + 16 * wave +
+                                                 4 * g) = to_four<T>(acc[j]);
   }
+  __syncthreads();
+  yst.take(ys, XS);
+  yst.put(y + start(count - 1) * sh.heads * P, sh.heads * P, tokens(count - 1), at.rows);
   if (d.fin && at.seg + 1 == sh.segs)
-    store_state<VEC>(s, d.fin + hd.at * size + tile, p, hd.rows, N);
+    store_state<VEC>(s, d.fin + at.at * size + tile, p, at.rows, N, t0);
 }
 
 // ------------------------------------------------------------ gradient
@@ -964,38 +1007,26 @@ __global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to
   if (i < count) to[i] = from ? from[i] : 0.0f;
 }
 
-template <typename T, int NT, bool VEC, int HB>
+template <typename T, int NT, bool VEC>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
   const ScanDir &d0 = d[0], &d1 = d[nd - 1];
-  const dim3 grid(sh.batch * sh.segs * (sh.heads * sh.ptiles / HB), 1, nd);
+  const dim3 grid(sh.batch * sh.segs * sh.heads * sh.ptiles, 1, nd);
   if (sh.segs > 1) {
-    k_scan_states<T, NT, VEC, HB><<<grid, 256 * HB, 0, s>>>(sh, d0, d1, true);
+    k_scan_states<T, NT, VEC><<<grid, kScanThreads, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
     const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
     k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
     if (hipError_t e = hipGetLastError()) return e;
   }
   if (!main) return hipSuccess;
-  k_scan_states<T, NT, VEC, HB><<<grid, 256 * HB, 0, s>>>(sh, d0, d1, false);
+  k_scan_states<T, NT, VEC><<<grid, kScanThreads, 0, s>>>(sh, d0, d1, false);
   return hipGetLastError();
-}
-template <typename T, int NT, bool VEC>
-hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
-  if constexpr (sizeof(T) == 2 && VEC)
-    if (sh.tiles == 2) return states<T, NT, VEC, 2>(sh, d, nd, main, s);
-  return states<T, NT, VEC, 1>(sh, d, nd, main, s);
 }
 template <typename T, int NT, bool VEC>
 hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
   if (hipError_t e = states<T, NT, VEC>(sh, &d, 1, false, s)) return e;
-  const uint32_t grid = sh.batch * sh.segs * (sh.heads * sh.ptiles / sh.tiles);
-  if constexpr (sizeof(T) == 2 && VEC) {
-    if (sh.tiles == 2) {
-      k_scan_out<T, NT, VEC, 2><<<grid, 512, 0, s>>>(sh, d, o);
-      return hipGetLastError();
-    }
-  }
-  k_scan_out<T, NT, VEC, 1><<<grid, 256, 0, s>>>(sh, d, o);
+  const uint32_t grid = sh.batch * sh.segs * sh.heads * sh.ptiles;
+  k_scan_out<T, NT, VEC><<<grid, kScanThreads, 0, s>>>(sh, d, o);
   return hipGetLastError();
 }
 

@@ -56,14 +56,17 @@ struct Rows {
   }
 };
 
-// Workgroups that a pass over the sequence should have: enough to occupy most
-// of the 256 compute units.
-constexpr uint64_t kWantedGroups = 192;
-
-// A workgroup carries the state of one channel tile from chunk to chunk.
-// Where there are too few tiles to fill the chip the sequence is cut into
-// segments of whole chunks, two at least (a segment's pass over its own tokens
-// is the price: x and B are read twice).  `dirs`: passes that run at once.
+// How a pass over the sequence is cut.  A workgroup carries the states of its
+// channel tiles from chunk to chunk.  With many tiles each takes its sequence as
+// a whole, in workgroups of eight waves.  With fewer the sequence is cut into
+// segments of whole chunks (a segment's pass over its own tokens is the price: x
+// and B are read twice): in workgroups of two tiles, which share what is read of
+// B and C, where segments of four chunks still fill the chip; of one tile and
+// shorter segments, two chunks at least, where they do not.
+// `dirs`: passes that run at once.
+constexpr uint64_t kWholeTiles = 160;   // tiles that occupy most of 256 compute units
+constexpr uint64_t kPairGroups = 512;   // workgroups of pairs, two on each unit
+constexpr uint64_t kShortGroups = 256;  // workgroups of one tile
 ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   ScanShape s{};
   s.batch = d->batch;
@@ -76,9 +79,18 @@ ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   s.la_batch = d->la_batch;
   s.chunks = (uint32_t)(((uint64_t)d->len + kChunk - 1) / kChunk);
   s.ptiles = (d->head_dim + kPTile - 1) / kPTile;
-  const uint64_t groups = (uint64_t)d->batch * d->heads * s.ptiles * dirs;
-  const uint64_t want = std::max<uint64_t>(1, groups ? kWantedGroups / groups : 1);
-  const uint64_t segs = std::min<uint64_t>(want, std::max<uint32_t>(1, s.chunks / 2));
+  const uint64_t tiles = (uint64_t)d->batch * d->heads * s.ptiles * dirs;
+  const bool pairs = d->dtype == FESC_BF16 && d->heads / d->groups * s.ptiles % 2 == 0;
+  uint64_t segs = 1;
+  s.tiles = 1;
+  if (tiles && tiles < kWholeTiles) {
+    if (pairs && tiles / 2 * (s.chunks / 4) >= kPairGroups) {
+      s.tiles = 2;
+      segs = kPairGroups / (tiles / 2);
+    } else {
+      segs = std::min<uint64_t>(kShortGroups / tiles, std::max<uint32_t>(1, s.chunks / 2));
+    }
+  }
   s.seg_chunks = (uint32_t)((s.chunks + segs - 1) / segs);
   s.segs = s.chunks ? (s.chunks + s.seg_chunks - 1) / s.seg_chunks : 1;
   return s;
@@ -234,6 +246,7 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(h0).add(hT).add(y).len(d->head_dim)
               .len(d->d_state).ok;
+  if (!s.vec) s.tiles = 1;
   dir.u = x;
   dir.v = B;
   dir.u_token = d->x_token;
@@ -268,6 +281,7 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(dy, d->dy_token, d->dy_batch).add(h0).add(dhT)
               .add(dh0).add(dx).add(db).add(dc).len(d->head_dim).len(d->d_state).ok;
+  if (!s.vec) s.tiles = 1;
   dir[0].u = x;
   dir[0].v = B;
   dir[0].u_token = d->x_token;

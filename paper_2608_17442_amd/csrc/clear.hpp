@@ -35,6 +35,7 @@ struct ScanShape {
   uint32_t seg_chunks;  // chunks per segment
   uint32_t segs;
   uint32_t ptiles;      // ceil(head_dim / kPTile)
+  uint32_t tiles;       // channel tiles in one workgroup: 1, or 2 (aligned bfloat16)
   const void* la;
   int64_t la_token, la_batch;
   bool vec;  // every row of every array starts at a multiple of 16 bytes

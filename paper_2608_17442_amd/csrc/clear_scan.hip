@@ -294,40 +294,63 @@ __device__ __forceinline__ Cum cumulate(float la) {
 
 // ------------------------------------------------------------ scan kernels
 
-// One workgroup: one channel tile of a head over the chunks of one segment.
-// Wave 4 e + w holds the state rows p = 16 w + l % 16, of them the entries n of
-// half e, as transposed MFMA result tiles t = e NT / 32 ... (e + 1) NT / 32 - 1
-// with n = state_col(t, g) + i (g = l / 16): tiles 2 q and 2 q + 1 together are, in
-// registers, the operand S[p][32 q + 8 g ...] of the product with C.  Eight
-// waves per head: what bounds these kernels is the time from chunk to chunk,
-// which halves with the work of each wave.
-constexpr int kScanThreads = 512;
-template <typename T, int NT>
+// One workgroup: HB neighbouring channel tiles (heads, where a head has one
+// tile) of one group over the chunks of one segment; what it reads of B and C
+// serves all of them.  Of each, wave 4 e + w (e < EW) holds the state rows
+// p = 16 w + l % 16, of them part e of the entries n, as transposed MFMA result
+// tiles t = e kOwn ... (e + 1) kOwn - 1 with n = state_col(t, g) + i (g = l / 16):
+// tiles 2 q and 2 q + 1 together are, in registers, the operand
+// S[p][32 q + 8 g ...] of the product with C.
+// The registers are held to two workgroups on a compute unit (in bfloat16: LDS
+// has no room for a second one in float32).
+// HB = 2, EW = 1 moves the least through LDS per head; HB = 1, EW = 2 takes the
+// least time from one chunk to the next.
+template <typename T, int NT, int HB, int EW>
 struct ScanTiles {
   static constexpr int XS = PT + Elem<T>::kPad;
   static constexpr int NS = NT + Elem<T>::kPad;
-  static constexpr int kOwn = NT / 32;  // state tiles of a wave
+  static constexpr int kThreads = 256 * EW;
+  static constexpr int kOwn = NT / 16 / EW;  // state tiles of a wave, per channel tile
 };
 
-// Heads that read the same B and C rows lie `batch * segs` workgroups apart:
-// on one XCD where that is a multiple of 8.
+// Workgroups that read the same B and C rows lie `batch * segs` apart: on one
+// XCD where that is a multiple of 8.
 struct Where {
-  uint32_t b, h, seg, g;
-  int p0, rows;  // first channel of the tile, its channels
-  uint64_t at;   // batch * heads + head
-  __device__ __forceinline__ explicit Where(const ScanShape& sh) {
-    const uint32_t per = sh.batch * sh.segs, bs = blockIdx.x % per, v = blockIdx.x / per;
-    b = bs / sh.segs;
-    seg = bs % sh.segs;
+  uint32_t b, v, seg, g;  // v: first channel tile, among those of all heads
+  template <int HB>
+  __device__ __forceinline__ static Where of(const ScanShape& sh) {
+    Where w;
+    const uint32_t per = sh.batch * sh.segs, bs = blockIdx.x % per;
+    w.b = bs / sh.segs;
+    w.seg = bs % sh.segs;
+    w.v = blockIdx.x / per * HB;
+    w.g = w.v / sh.ptiles / (sh.heads / sh.groups);
+    return w;
+  }
+};
+// The channel tile whose running sums a wave forms, -1: none.  Of the output
+// kernel's waves these have least to do with G.
+template <int HB, int EW>
+__device__ __forceinline__ int sums_tile() {
+  const int h = wave_id() - 4 * (EW - 1);
+  return h >= 0 && h < HB ? h : -1;
+}
+
+// One channel tile of a workgroup.
+struct Head {
+  uint32_t h;     // head
+  int p0, rows;   // first channel, channels
+  uint64_t at;    // batch * heads + head
+  __device__ __forceinline__ Head(const ScanShape& sh, const Where& w, int k) {
+    const uint32_t v = w.v + k;
     h = v / sh.ptiles;
-    g = h / (sh.heads / sh.groups);
     p0 = v % sh.ptiles * PT;
     rows = min(PT, (int)sh.head_dim - p0);
-    at = (uint64_t)b * sh.heads + h;
+    at = (uint64_t)w.b * sh.heads + h;
   }
 };
 
-// Tiles t0 ... of the state from and to memory.
+// A wave's part of a state, tiles t0 ..., from and to memory.
 template <bool VEC, int NTILES>
 __device__ __forceinline__ void load_state(f32x4 (&s)[NTILES], const float* base, int p, int rows,
                                            int N, int t0) {
@@ -344,10 +367,19 @@ __device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], T* base, i
                                             int N, int t0) {
   const int g = (threadIdx.x & 63) >> 4;
   const Mem m(base);
+  if constexpr (VEC && sizeof(T) == 2) {  // two tiles side by side: eight entries at once
 #pragma unroll
-  for (int t = 0; t < NTILES; ++t) {
-    const int n = state_col(t0 + t, g);
-    m.store_four<T, VEC>((p * N + n) * (uint32_t)sizeof(T), s[t], p < rows ? N - n : 0);
+    for (int t = 0; t < NTILES; t += 2) {
+      const int n = state_col(t0 + t, g);
+      m.store16(p < rows && n < N ? (p * N + n) * 2u : kAbsent,
+                __builtin_bit_cast(u32x4, join(to_four<T>(s[t]), to_four<T>(s[t + 1]))));
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < NTILES; ++t) {
+      const int n = state_col(t0 + t, g);
+      m.store_four<T, VEC>((p * N + n) * (uint32_t)sizeof(T), s[t], p < rows ? N - n : 0);
+    }
   }
 }
 
@@ -368,24 +400,31 @@ __device__ __forceinline__ f32x4 half(const f32x8& v, int k) {
 }
 
 // S' = total S + sum_r w_r x_r B_r^T over the chunk in LDS; xf: this wave's rows
-// of x as operands.  Two tiles at a time, whose products do not wait for each
-// other's sums.
-template <typename T, int NT>
-__device__ __forceinline__ void update_state(f32x4 (&s)[NT / 32],
-                                             const typename Elem<T>::Frag (&xf)[2], const T* bs,
-                                             const float* w, float total, int t0) {
-  constexpr int NS = ScanTiles<T, NT>::NS;
+// of x as operands.  Two state tiles at a time, whose products do not wait for
+// each other's sums.
+template <typename T, int NT, int HB, int OWN>
+__device__ __forceinline__ void update_state(f32x4 (&s)[HB][OWN],
+                                             const typename Elem<T>::Frag (&xf)[HB][2],
+                                             const T* bs, const float (&w)[HB][Q],
+                                             const float (&total)[HB], int t0) {
+  constexpr int NS = NT + Elem<T>::kPad;
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int t = 0; t < NT / 32; ++t) s[t] *= total;
+  for (int h = 0; h < HB; ++h) {
+    const float e = total[h];
+#pragma unroll
+    for (int t = 0; t < OWN; ++t) s[h][t] *= e;
+  }
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int r = 32 * q + 4 * g;
-    Parts<T> x;
-    x.split(half(xf[q], 0) * *reinterpret_cast<const f32x4*>(w + r),
-            half(xf[q], 1) * *reinterpret_cast<const f32x4*>(w + r + 16));
+    Parts<T> x[HB];
 #pragma unroll
-    for (int t = 0; t < NT / 32; t += 2) {
+    for (int h = 0; h < HB; ++h)
+      x[h].split(half(xf[h][q], 0) * *reinterpret_cast<const f32x4*>(w[h] + r),
+                 half(xf[h][q], 1) * *reinterpret_cast<const f32x4*>(w[h] + r + 16));
+#pragma unroll
+    for (int t = 0; t < OWN; t += 2) {
       typename Elem<T>::Frag b[2];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
@@ -393,7 +432,10 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[NT / 32],
 #pragma unroll
       for (int k = 0; k < Parts<T>::kCount; ++k) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f) s[t + f] = mma(b[f], x.p[k], s[t + f]);
+        for (int h = 0; h < HB; ++h) {
+#pragma unroll
+          for (int f = 0; f < 2; ++f) s[h][t + f] = mma(b[f], x[h].p[k], s[h][t + f]);
+        }
       }
     }
   }
@@ -403,83 +445,110 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[NT / 32],
 // zero, and its total decay, to seg_states and seg_decay.  Otherwise from the
 // state that enters the segment: the states that enter the chunks, and the
 // final state.  Chunks lie in LDS in turn in two places: one barrier each.
-template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kScanThreads, 2) void k_scan_states(ScanShape sh, ScanDir d0,
-                                                                 ScanDir d1, bool summaries) {
-  using Tiles = ScanTiles<T, NT>;
+template <typename T, int NT, bool VEC, int HB, int EW>
+__global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_scan_states(
+    ScanShape sh, ScanDir d0, ScanDir d1, bool summaries) {
+  using Tiles = ScanTiles<T, NT, HB, EW>;
+  constexpr int kThreads = Tiles::kThreads;
   constexpr int XS = Tiles::XS, NS = Tiles::NS;
-  __shared__ __align__(16) T xs[2][Q * XS];
+  __shared__ __align__(16) T xs[2][HB][Q * XS];
   __shared__ __align__(16) T bs[2][Q * NS];
-  __shared__ __align__(16) float wt[2][Q];
-  __shared__ float total[2];
+  __shared__ __align__(16) float wt[2][HB][Q];
+  __shared__ float total[2][HB];
   const ScanDir& d = blockIdx.z ? d1 : d0;
-  const Where at(sh);
-  const int wave = wave_id() & 3, t0 = (wave_id() >> 2) * Tiles::kOwn, lane = threadIdx.x & 63;
+  const Where at = Where::of<HB>(sh);
+  const int wave = wave_id() & 3, part = wave_id() >> 2, t0 = part * Tiles::kOwn;
+  const int lane = threadIdx.x & 63;
+  const int sums_of = sums_tile<HB, EW>();  // whose running sums this wave forms
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + (lane & 15);
   // segments and chunks are counted in the direction of the pass
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
   if (summaries && at.seg + 1 == sh.segs) return;  // no segment follows the last
-  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)at.p0 * N;
-  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + at.p0;
+  const uint64_t size = (uint64_t)P * N;
+  const T* u = (const T*)d.u + at.b * d.u_batch;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + Head(sh, at, sums_of < 0 ? 0 : sums_of).h;
 
-  f32x4 s[Tiles::kOwn];
-  const float* from = summaries      ? nullptr
-                      : d.seg_states ? d.seg_states + (at.at * sh.segs + at.seg) * size
-                      : d.init       ? d.init + at.at * size
-                                     : nullptr;
-  if (from) {
-    load_state<VEC>(s, from + tile, p, at.rows, N, t0);
-  } else {
+  f32x4 s[HB][Tiles::kOwn];
 #pragma unroll
-    for (int t = 0; t < Tiles::kOwn; ++t) s[t] = f32x4{0, 0, 0, 0};
+  for (int h = 0; h < HB; ++h) {
+    const Head hd(sh, at, h);
+    const float* from = summaries      ? nullptr
+                        : d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
+                        : d.init       ? d.init + hd.at * size
+                                       : nullptr;
+    if (from) {
+      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
+    } else {
+#pragma unroll
+      for (int t = 0; t < Tiles::kOwn; ++t) s[h][t] = f32x4{0, 0, 0, 0};
+    }
   }
-  Stage<T, Q, PT, kScanThreads, VEC> xst;
-  Stage<T, Q, NT, kScanThreads, VEC> bst;
-  float lav = 0.0f;  // wave 0: log decay of token `lane`
+  Stage<T, Q, PT, kThreads, VEC> xst[HB];
+  Stage<T, Q, NT, kThreads, VEC> bst;
+  float lav = 0.0f;  // log decay of token `lane` of that tile
   auto chunk = [&](int k) { return d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k; };
   auto fetch = [&](int k) {
-    const int64_t from = (int64_t)chunk(k) * Q;
-    const int n = min((int64_t)Q, (int64_t)sh.len - from);
-    if (wave_id() == 0)
-      lav = Mem(la + from * sh.la_token)
+    const int64_t start = (int64_t)chunk(k) * Q;
+    const int n = min((int64_t)Q, (int64_t)sh.len - start);
+    if (sums_of >= 0)
+      lav = Mem(la + start * sh.la_token)
                 .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
-    xst.load(u + from * d.u_token, d.u_token, n, at.rows);
-    bst.load(v + from * d.v_token, d.v_token, n, N);
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      const Head hd(sh, at, h);
+      xst[h].load(u + start * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+    }
+    bst.load(v + start * d.v_token, d.v_token, n, N);
   };
   auto place = [&](int k) {
-    xst.store(xs[k & 1], XS);
-    bst.store(bs[k & 1], NS);
-    if (wave_id() == 0) {
+    if (sums_of >= 0) {
       const Cum cum = cumulate(lav);
-      wt[k & 1][lane] = d.reverse ? cum.e : cum.w;
-      if (lane == 0) total[k & 1] = cum.total;
+      wt[k & 1][sums_of][lane] = d.reverse ? cum.e : cum.w;
+      if (lane == 0) total[k & 1][sums_of] = cum.total;
     }
+#pragma unroll
+    for (int h = 0; h < HB; ++h) xst[h].store(xs[k & 1][h], XS);
+    bst.store(bs[k & 1], NS);
     __syncthreads();
   };
   fetch(0);
   place(0);
-  float decay = 1.0f;
+  float decay[HB];
+#pragma unroll
+  for (int h = 0; h < HB; ++h) decay[h] = 1.0f;
   for (int k = 0; k < count; ++k) {
     if (k + 1 < count) fetch(k + 1);
-    if (d.chunk_states && !summaries)
-      store_state<VEC>(s, (T*)d.chunk_states + (at.at * sh.chunks + chunk(k)) * size + tile, p,
-                       at.rows, N, t0);
-    typename Elem<T>::Frag xf[2];
+    if (d.chunk_states && !summaries) {
 #pragma unroll
-    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs[k & 1], XS, q, 16 * wave);
-    decay *= total[k & 1];
-    update_state<T, NT>(s, xf, bs[k & 1], wt[k & 1], total[k & 1], t0);
+      for (int h = 0; h < HB; ++h) {
+        const Head hd(sh, at, h);
+        store_state<VEC>(s[h], (T*)d.chunk_states + (hd.at * sh.chunks + chunk(k)) * size +
+                                   (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
+      }
+    }
+    typename Elem<T>::Frag xf[HB][2];
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[k & 1][h], XS, q, 16 * wave);
+      decay[h] *= total[k & 1][h];
+    }
+    update_state<T, NT, HB>(s, xf, bs[k & 1], wt[k & 1], total[k & 1], t0);
     if (k + 1 < count) place(k + 1);
   }
-  if (summaries) {
-    store_state<VEC>(s, d.seg_states + (at.at * sh.segs + at.seg + 1) * size + tile, p, at.rows, N,
-                     t0);
-    if (threadIdx.x == 0 && at.p0 == 0) d.seg_decay[at.at * sh.segs + at.seg] = decay;
-  } else if (d.fin && at.seg + 1 == sh.segs) {
-    store_state<VEC>(s, d.fin + at.at * size + tile, p, at.rows, N, t0);
+#pragma unroll
+  for (int h = 0; h < HB; ++h) {
+    const Head hd(sh, at, h);
+    const uint64_t tile = (uint64_t)hd.p0 * N;
+    if (summaries) {
+      store_state<VEC>(s[h], d.seg_states + (hd.at * sh.segs + at.seg + 1) * size + tile, p,
+                       hd.rows, N, t0);
+      if (threadIdx.x == 0 && hd.p0 == 0) d.seg_decay[hd.at * sh.segs + at.seg] = decay[h];
+    } else if (d.fin && at.seg + 1 == sh.segs) {
+      store_state<VEC>(s[h], d.fin + hd.at * size + tile, p, hd.rows, N, t0);
+    }
   }
 }
 
@@ -503,63 +572,70 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
 }
 
 // Outputs and final state.  Per chunk: wave 4 e + w forms the columns of token
-// tile w of G^T, G = C B^T, for the tokens r of half e, and writes their product
-// with the decays to LDS; then y^T for its 16 channels and the tokens of half e
-// from that, x and the state (its own half of it from the registers, the other
-// through LDS), and updates its part of the state.
-template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(kScanThreads, sizeof(T) == 2 ? 4 : 2) void k_scan_out(ScanShape sh,
-                                                                                   ScanDir d,
-                                                                                   ScanOut o) {
-  using Tiles = ScanTiles<T, NT>;
+// tile w of G^T, G = C B^T, once for the HB tiles (the tokens r of half e where
+// EW = 2), and writes their products with each tile's decays to LDS; meanwhile the
+// state's part of y^T for its 16 channels and all tokens (half e), and its part
+// of the new state; then the chunk's own part of y^T from what all waves wrote.
+template <typename T, int NT, bool VEC, int HB, int EW>
+__global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_scan_out(
+    ScanShape sh, ScanDir d, ScanOut o) {
+  using Tiles = ScanTiles<T, NT, HB, EW>;
+  constexpr int kThreads = Tiles::kThreads;
   constexpr int XS = Tiles::XS, NS = Tiles::NS;
-  constexpr int NQ = NT / 32, HQ = NT / 64;  // operands of the state, and of half of it
-  __shared__ __align__(16) T xs[Q * XS];
+  constexpr int NQ = NT / 32, kTokenTiles = 4 / EW;
+  __shared__ __align__(16) T xs[HB][Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
-  __shared__ __align__(16) T lg[Q * XS];
-  __shared__ __align__(16) T ys[Q * XS];
-  __shared__ __align__(16) T ss[NQ][PT * 32];  // the state's operands, lane by lane
-  __shared__ __align__(16) float hi[2][Q], lo[2][Q], ec[2][Q], wt[2][Q];
-  __shared__ float total[2];
+  __shared__ __align__(16) T lg[HB][Q * XS];
+  // the state's operands, lane by lane, where a wave holds only some of them
+  __shared__ __align__(16) T ss[EW > 1 ? HB * NQ : 1][EW > 1 ? PT * 32 : 8];
+  __shared__ __align__(16) float hi[2][HB][Q], lo[2][HB][Q], wt[2][HB][Q];
+  __shared__ float total[2][HB];
   using Frag = typename Elem<T>::Frag;
-  const Where at(sh);
-  const int id = wave_id(), wave = id & 3, e = id >> 2, t0 = e * Tiles::kOwn;
+  const Where at = Where::of<HB>(sh);
+  const int sums_of = sums_tile<HB, EW>();
+  const int wave = wave_id() & 3, part = wave_id() >> 2, t0 = part * Tiles::kOwn;
   const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + col;
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
-  const uint64_t size = (uint64_t)P * N, tile = (uint64_t)at.p0 * N;
-  const T* u = (const T*)d.u + at.b * d.u_batch + (int64_t)at.h * P + at.p0;
+  const uint64_t size = (uint64_t)P * N;
+  const T* u = (const T*)d.u + at.b * d.u_batch;
   const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
   const T* cc = (const T*)o.c + at.b * o.c_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch + at.h;
-  T* y = (T*)o.y + ((uint64_t)at.b * sh.len * sh.heads + at.h) * P + at.p0;
+  const T* la = (const T*)sh.la + at.b * sh.la_batch + Head(sh, at, sums_of < 0 ? 0 : sums_of).h;
 
-  f32x4 s[Tiles::kOwn];
-  const float* from = d.seg_states ? d.seg_states + (at.at * sh.segs + at.seg) * size
-                      : d.init     ? d.init + at.at * size
-                                   : nullptr;
-  if (from) {
-    load_state<VEC>(s, from + tile, p, at.rows, N, t0);
-  } else {
+  f32x4 s[HB][Tiles::kOwn];
 #pragma unroll
-    for (int t = 0; t < Tiles::kOwn; ++t) s[t] = f32x4{0, 0, 0, 0};
+  for (int h = 0; h < HB; ++h) {
+    const Head hd(sh, at, h);
+    const float* from = d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
+                        : d.init     ? d.init + hd.at * size
+                                     : nullptr;
+    if (from) {
+      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
+    } else {
+#pragma unroll
+      for (int t = 0; t < Tiles::kOwn; ++t) s[h][t] = f32x4{0, 0, 0, 0};
+    }
   }
-  Stage<T, Q, PT, kScanThreads, VEC> xst, yst;
-  Stage<T, Q, NT, kScanThreads, VEC> bst, cst;
+  Stage<T, Q, PT, kThreads, VEC> xst[HB];
+  Stage<T, Q, NT, kThreads, VEC> bst, cst;
   auto start = [&](int k) { return (int64_t)(first + k) * Q; };
   auto tokens = [&](int k) { return (int)min((int64_t)Q, (int64_t)sh.len - start(k)); };
   auto fetch = [&](int k) {
     const int n = tokens(k);
     bst.load(v + start(k) * d.v_token, d.v_token, n, N);
     cst.load(cc + start(k) * o.c_token, o.c_token, n, N);
-    xst.load(u + start(k) * d.u_token, d.u_token, n, at.rows);
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      const Head hd(sh, at, h);
+      xst[h].load(u + start(k) * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+    }
   };
-  // Running sums of chunk k, by the wave that has least of G: two chunks ahead
-  // from memory, one ahead into LDS.
-  constexpr int kSums = 4;
-  float lav = 0.0f;  // log decay of token `lane`
+  // Log decays come two chunks ahead from memory, their running sums one ahead
+  // into LDS.
+  float lav = 0.0f;
   auto fetch_la = [&](int k) {
     if (k < count)
       lav = Mem(la + start(k) * sh.la_token)
@@ -568,105 +644,161 @@ __global__ __launch_bounds__(kScanThreads, sizeof(T) == 2 ? 4 : 2) void k_scan_o
   };
   auto sums = [&](int k) {
     const Cum cum = cumulate(lav);
-    hi[k & 1][lane] = cum.hi;
-    lo[k & 1][lane] = cum.lo;
-    ec[k & 1][lane] = cum.e;
-    wt[k & 1][lane] = cum.w;
-    if (lane == 0) total[k & 1] = cum.total;
+    hi[k & 1][sums_of][lane] = cum.hi;
+    lo[k & 1][sums_of][lane] = cum.lo;
+    wt[k & 1][sums_of][lane] = cum.w;
+    if (lane == 0) total[k & 1][sums_of] = cum.total;
+  };
+  // Outputs of a chunk, which lie in LDS in the place of its x, to memory.
+  auto put_y = [&](int k) {
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      const Head hd(sh, at, h);
+      Stage<T, Q, PT, kThreads, VEC> y;
+      y.take(xs[h], XS);
+      y.put((T*)o.y + (((uint64_t)at.b * sh.len + start(k)) * sh.heads + hd.h) * P + hd.p0,
+            sh.heads * P, tokens(k), hd.rows);
+    }
   };
   fetch(0);
-  if (id == kSums) {
+  if (sums_of >= 0) {
     fetch_la(0);
     sums(0);
     fetch_la(1);
   }
-  // Two barriers a chunk.  Between the first and the second the tiles of the
-  // chunk, the state's operands and the outputs of the chunk before are read and
-  // lg is written; after the second lg is read and the tiles, operands and
-  // outputs are written.
   for (int k = 0; k < count; ++k) {
     const int now = k & 1;
+    if (k) {
+      __syncthreads();
+      put_y(k - 1);
+    }
+    // a thread stores its x where it has read outputs
+#pragma unroll
+    for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
     bst.store(bs, NS);
     cst.store(cs, NS);
-    xst.store(xs, XS);
-    Frag sf[NQ];
+    if constexpr (EW > 1) {
 #pragma unroll
-    for (int q = 0; q < HQ; ++q) {
-      const Frag f = join(to_four<T>(s[2 * q]), to_four<T>(s[2 * q + 1]));
-      *reinterpret_cast<Frag*>(ss[e * HQ + q] + (64 * wave + lane) * 8) = f;
+      for (int h = 0; h < HB; ++h) {
+#pragma unroll
+        for (int t = 0; t < Tiles::kOwn; t += 2)
+          *reinterpret_cast<Frag*>(ss[h * NQ + (t0 + t) / 2] + (64 * wave + lane) * 8) =
+              join(to_four<T>(s[h][t]), to_four<T>(s[h][t + 1]));
+      }
     }
     __syncthreads();
     if (k + 1 < count) fetch(k + 1);
-    if (k) {
-      yst.take(ys, XS);
-      yst.put(y + start(k - 1) * sh.heads * P, sh.heads * P, tokens(k - 1), at.rows);
-    }
-    if (id == kSums && k + 1 < count) {
+    if (sums_of >= 0 && k + 1 < count) {
       sums(k + 1);
       fetch_la(k + 2);
     }
-    if (2 * e <= wave) {
-      // rows r = 32 e + 16 f + 4 g + i, column s = 16 wave + col
-      f32x4 gt[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    {
+      // rows r = 16 j + 4 g + i, column s = 16 wave + col
+      Frag cf[NQ];
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const Frag cf = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
+      for (int q = 0; q < NQ; ++q)
+        cf[q] = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
-          gt[f] = mma(row_frag(bs + (32 * e + 16 * f + col) * NS + 32 * q + 8 * g), cf, gt[f]);
+      for (int e0 = 0; e0 < 2 / EW; ++e0) {
+        const int e = EW > 1 ? part : e0;
+        if (2 * e > wave) break;
+        f32x4 gt[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+          for (int f = 0; f < 2; ++f)
+            gt[f] = mma(row_frag(bs + (32 * e + 16 * f + col) * NS + 32 * q + 8 * g), cf[q], gt[f]);
+        }
+#pragma unroll
+        for (int h = 0; h < HB; ++h) {
+          const float hs = hi[now][h][16 * wave + col], ls = lo[now][h][16 * wave + col];
+          f32x4 w[2];
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            const int r = 32 * e + 16 * f + 4 * g;
+            const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[now][h] + r);
+            const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[now][h] + r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[f][i] = gt[f][i] * exp2_seen(r + i <= 16 * wave + col, hs, ls, hr[i], lr[i]);
+          }
+          // position 32 q + 8 g + 4 f + i holds token 32 q + 16 f + 4 g + i, so that
+          // a row read gives the operand that matches token_frag
+          *reinterpret_cast<Frag*>(lg[h] + (16 * wave + col) * XS + 32 * e + 8 * g) =
+              join(to_four<T>(w[0]), to_four<T>(w[1]));
+        }
       }
-      const float hs = hi[now][16 * wave + col], ls = lo[now][16 * wave + col];
-      f32x4 w[2];
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int r = 32 * e + 16 * f + 4 * g;
-        const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[now] + r);
-        const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[now] + r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w[f][i] = gt[f][i] * exp2_seen(r + i <= 16 * wave + col, hs, ls, hr[i], lr[i]);
-      }
-      // position 32 q + 8 g + 4 f + i holds token 32 q + 16 f + 4 g + i, so that a
-      // row read gives the operand that matches token_frag
-      *reinterpret_cast<Frag*>(lg + (16 * wave + col) * XS + 32 * e + 8 * g) =
-          join(to_four<T>(w[0]), to_four<T>(w[1]));
     }
-    Frag xf[2];
+    Frag xf[HB][2];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) xf[q] = token_frag(xs, XS, q, 16 * wave);
+    for (int h = 0; h < HB; ++h) {
 #pragma unroll
-    for (int q = 0; q < NQ; ++q)
-      sf[q] = *reinterpret_cast<const Frag*>(ss[q] + (64 * wave + lane) * 8);
-    // y^T: rows p = 16 wave + 4 g + i, columns s = 32 e + 16 j + col
-    f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+      for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[h], XS, q, 16 * wave);
+    }
+    // y^T: rows p = 16 wave + 4 g + i, columns s = 16 (j0 + j) + col
+    const int j0 = kTokenTiles * part;
+    f32x4 acc[HB][kTokenTiles];
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+#pragma unroll
+      for (int j = 0; j < kTokenTiles; ++j) acc[h][j] = f32x4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
+      Frag sf[HB];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        acc[j] = mma(sf[q], row_frag(cs + (32 * e + 16 * j + col) * NS + 32 * q + 8 * g), acc[j]);
+      for (int h = 0; h < HB; ++h) {
+        if constexpr (EW > 1)
+          sf[h] = *reinterpret_cast<const Frag*>(ss[h * NQ + q] + (64 * wave + lane) * 8);
+        else
+          sf[h] = join(to_four<T>(s[h][2 * q]), to_four<T>(s[h][2 * q + 1]));
+      }
+#pragma unroll
+      for (int j = 0; j < kTokenTiles; ++j) {
+        const Frag cf = row_frag(cs + (16 * (j0 + j) + col) * NS + 32 * q + 8 * g);
+#pragma unroll
+        for (int h = 0; h < HB; ++h) acc[h][j] = mma(sf[h], cf, acc[h][j]);
+      }
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) acc[j] *= ec[now][32 * e + 16 * j + col];
-    update_state<T, NT>(s, xf, bs, wt[now], total[now], t0);
+    for (int h = 0; h < HB; ++h) {
+#pragma unroll
+      for (int j = 0; j < kTokenTiles; ++j) {
+        const int s16 = 16 * (j0 + j) + col;
+        acc[h][j] *= exp2_diff(hi[now][h][s16], lo[now][h][s16], 0.0f, 0.0f);
+      }
+    }
+    update_state<T, NT, HB>(s, xf, bs, wt[now], total[now], t0);
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      if (q <= e) {
+      if (EW > 1 && q > part) break;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[j] = mma(xf[q], row_frag(lg + (32 * e + 16 * j + col) * XS + 32 * q + 8 * g), acc[j]);
+      for (int h = 0; h < HB; ++h) {
+#pragma unroll
+        for (int j = EW > 1 ? 0 : 2 * q; j < kTokenTiles; ++j)
+          acc[h][j] = mma(xf[h][q], row_frag(lg[h] + (16 * (j0 + j) + col) * XS + 32 * q + 8 * g),
+                          acc[h][j]);
       }
     }
+    // over x, of which every wave has read what it needs
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      *reinterpret_cast<typename Elem<T>::Four*>(ys + (32 * e + 16 * j + col) * XS + 16 * wave +
-                                                 4 * g) = to_four<T>(acc[j]);
+    for (int h = 0; h < HB; ++h) {
+#pragma unroll
+      for (int j = 0; j < kTokenTiles; ++j)
+        *reinterpret_cast<typename Elem<T>::Four*>(xs[h] + (16 * (j0 + j) + col) * XS + 16 * wave +
+                                                   4 * g) = to_four<T>(acc[h][j]);
+    }
   }
   __syncthreads();
-  yst.take(ys, XS);
-  yst.put(y + start(count - 1) * sh.heads * P, sh.heads * P, tokens(count - 1), at.rows);
-  if (d.fin && at.seg + 1 == sh.segs)
-    store_state<VEC>(s, d.fin + at.at * size + tile, p, at.rows, N, t0);
+  put_y(count - 1);
+  if (d.fin && at.seg + 1 == sh.segs) {
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+      const Head hd(sh, at, h);
+      store_state<VEC>(s[h], d.fin + hd.at * size + (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
+    }
+  }
 }
 
 // ------------------------------------------------------------ gradient
@@ -685,7 +817,7 @@ __global__ __launch_bounds__(kScanThreads, sizeof(T) == 2 ? 4 : 2) void k_scan_o
 // waves 4..7 hold 16 tokens of dC and dB.
 template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
-  constexpr int XS = ScanTiles<T, NT>::XS, NS = ScanTiles<T, NT>::NS;
+  constexpr int XS = PT + Elem<T>::kPad, NS = NT + Elem<T>::kPad;
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
   __shared__ __align__(16) T xs[Q * XS];
@@ -1007,27 +1139,39 @@ __global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to
   if (i < count) to[i] = from ? from[i] : 0.0f;
 }
 
-template <typename T, int NT, bool VEC>
+template <typename T, int NT, bool VEC, int HB, int EW>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
   const ScanDir &d0 = d[0], &d1 = d[nd - 1];
-  const dim3 grid(sh.batch * sh.segs * sh.heads * sh.ptiles, 1, nd);
+  const dim3 grid(sh.batch * sh.segs * (sh.heads * sh.ptiles / HB), 1, nd);
   if (sh.segs > 1) {
-    k_scan_states<T, NT, VEC><<<grid, kScanThreads, 0, s>>>(sh, d0, d1, true);
+    k_scan_states<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
     const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
     k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
     if (hipError_t e = hipGetLastError()) return e;
   }
   if (!main) return hipSuccess;
-  k_scan_states<T, NT, VEC><<<grid, kScanThreads, 0, s>>>(sh, d0, d1, false);
+  k_scan_states<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, false);
+  return hipGetLastError();
+}
+template <typename T, int NT, bool VEC, int HB, int EW>
+hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
+  if (hipError_t e = states<T, NT, VEC, HB, EW>(sh, &d, 1, false, s)) return e;
+  const uint32_t grid = sh.batch * sh.segs * (sh.heads * sh.ptiles / HB);
+  k_scan_out<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d, o);
   return hipGetLastError();
 }
 template <typename T, int NT, bool VEC>
+hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && VEC)
+    if (sh.tiles == 2) return states<T, NT, VEC, 2, 1>(sh, d, nd, true, s);
+  return states<T, NT, VEC, 1, 2>(sh, d, nd, true, s);
+}
+template <typename T, int NT, bool VEC>
 hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
-  if (hipError_t e = states<T, NT, VEC>(sh, &d, 1, false, s)) return e;
-  const uint32_t grid = sh.batch * sh.segs * sh.heads * sh.ptiles;
-  k_scan_out<T, NT, VEC><<<grid, kScanThreads, 0, s>>>(sh, d, o);
-  return hipGetLastError();
+  if constexpr (sizeof(T) == 2 && VEC)
+    if (sh.tiles == 2) return outputs<T, NT, VEC, 2, 1>(sh, d, o, s);
+  return outputs<T, NT, VEC, 1, 2>(sh, d, o, s);
 }
 
 // One instance per element type, padded state size and alignment.
@@ -1041,7 +1185,7 @@ hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipS
 
 hipError_t launch_scan_states(uint32_t dtype, const ScanShape& sh, const ScanDir* d, int nd,
                               hipStream_t s) {
-#define CALL(T, NT, VEC) states<T, NT, VEC>(sh, d, nd, true, s)
+#define CALL(T, NT, VEC) states<T, NT, VEC>(sh, d, nd, s)
   return FESC_SCAN_CASES(dtype, sh, CALL);
 #undef CALL
 }

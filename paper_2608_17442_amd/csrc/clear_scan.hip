@@ -150,32 +150,52 @@ __device__ __forceinline__ float load1(const T* p) {
   return (float)*p;
 }
 
+// Where a thread's units of a ROWS x COLS tile lie in memory.  VEC: rows start
+// at multiples of 16 bytes and do not overlap, so that one offset, formed once,
+// and the bytes that the valid rows span say all.
+template <typename T, int COLS, int THREADS, bool VEC>
+struct Rows {
+  uint32_t pitch, first, step;
+  int cols;
+  __device__ __forceinline__ Rows(uint32_t pitch_, int cols_) : pitch(pitch_), cols(cols_) {
+    constexpr int kUnit = Elem<T>::kUnit, kPerRow = COLS / kUnit;
+    const int row = threadIdx.x / kPerRow, col = threadIdx.x % kPerRow * kUnit;
+    first = col < cols ? (row * pitch + col) * (uint32_t)sizeof(T) : kAbsent;
+    step = THREADS / kPerRow * pitch * (uint32_t)sizeof(T);
+  }
+  __device__ __forceinline__ uint32_t bytes(int rows) const {
+    return ((rows - 1) * pitch + cols) * (uint32_t)sizeof(T);
+  }
+};
+
 // Registers of one thread for a tile of ROWS x COLS elements on its way from
-// global memory to LDS; rows and columns past the valid ones are zero.  VEC:
-// rows start at multiples of 16 bytes.
+// global memory to LDS; rows and columns past the valid ones are zero.
 template <typename T, int ROWS, int COLS, int THREADS, bool VEC>
 struct Stage {
   static constexpr int kUnit = Elem<T>::kUnit;
   static constexpr int kPerRow = COLS / kUnit;
   static constexpr int kUnits = ROWS * kPerRow / THREADS;
   static_assert(ROWS * kPerRow % THREADS == 0, "whole units per thread");
+  using In = Rows<T, COLS, THREADS, VEC>;
   u32x4 r[kUnits];
 
-  __device__ __forceinline__ void load(const T* base, uint32_t pitch, int rows, int cols) {
-    const Mem m(base);
+  __device__ __forceinline__ void load(const T* base, const In& in, int rows) {
+    if constexpr (VEC) {
+      const Mem m(base, in.bytes(rows));
 #pragma unroll
-    for (int k = 0; k < kUnits; ++k) {
-      const int i = threadIdx.x + k * THREADS;
-      const int row = i / kPerRow, col = i % kPerRow * kUnit;
-      const uint32_t at = (row * pitch + col) * (uint32_t)sizeof(T);
-      if constexpr (VEC) {
-        r[k] = m.load16(row < rows && col < cols ? at : kAbsent);
-      } else {
+      for (int k = 0; k < kUnits; ++k) r[k] = m.load16(in.first, k * in.step);
+    } else {
+      const Mem m(base);
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        const int row = i / kPerRow, col = i % kPerRow * kUnit;
+        const uint32_t at = (row * in.pitch + col) * (uint32_t)sizeof(T);
         u32x4 v = {0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < kUnit; ++j) {
-          const uint32_t w =
-              m.load_bits<T>(row < rows && col + j < cols ? at + j * (uint32_t)sizeof(T) : kAbsent);
+          const uint32_t w = m.load_bits<T>(
+              row < rows && col + j < in.cols ? at + j * (uint32_t)sizeof(T) : kAbsent);
           if constexpr (sizeof(T) == 4)
             v[j] = w;
           else
@@ -199,19 +219,21 @@ struct Stage {
       r[k] = *reinterpret_cast<const u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit);
     }
   }
-  __device__ __forceinline__ void put(T* base, uint32_t pitch, int rows, int cols) const {
-    const Mem m(base);
+  __device__ __forceinline__ void put(T* base, const In& out, int rows) const {
+    if constexpr (VEC) {
+      const Mem m(base, out.bytes(rows));
 #pragma unroll
-    for (int k = 0; k < kUnits; ++k) {
-      const int i = threadIdx.x + k * THREADS;
-      const int row = i / kPerRow, col = i % kPerRow * kUnit;
-      const uint32_t at = (row * pitch + col) * (uint32_t)sizeof(T);
-      if constexpr (VEC) {
-        m.store16(row < rows && col < cols ? at : kAbsent, r[k]);
-      } else {
+      for (int k = 0; k < kUnits; ++k) m.store16(out.first, r[k], k * out.step);
+    } else {
+      const Mem m(base);
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) {
+        const int i = threadIdx.x + k * THREADS;
+        const int row = i / kPerRow, col = i % kPerRow * kUnit;
+        const uint32_t at = (row * out.pitch + col) * (uint32_t)sizeof(T);
 #pragma unroll
         for (int j = 0; j < kUnit; ++j)
-          m.store_bits<T>(row < rows && col + j < cols ? at + j * (uint32_t)sizeof(T) : kAbsent,
+          m.store_bits<T>(row < rows && col + j < out.cols ? at + j * (uint32_t)sizeof(T) : kAbsent,
                           sizeof(T) == 4 ? r[k][j * sizeof(T) / 4]
                                          : r[k][j * sizeof(T) / 4] >> (16 * (j & 1)) & 0xffffu);
       }
@@ -485,22 +507,26 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
       for (int t = 0; t < Tiles::kOwn; ++t) s[h][t] = f32x4{0, 0, 0, 0};
     }
   }
-  Stage<T, Q, PT, kThreads, VEC> xst[HB];
-  Stage<T, Q, NT, kThreads, VEC> bst;
+  using XStage = Stage<T, Q, PT, kThreads, VEC>;
+  using NStage = Stage<T, Q, NT, kThreads, VEC>;
+  XStage xst[HB];
+  NStage bst;
+  const typename NStage::In bin(d.v_token, N);
   float lav = 0.0f;  // log decay of token `lane` of that tile
+  const uint32_t la_at = lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T);
   auto chunk = [&](int k) { return d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k; };
   auto fetch = [&](int k) {
     const int64_t start = (int64_t)chunk(k) * Q;
     const int n = min((int64_t)Q, (int64_t)sh.len - start);
     if (sums_of >= 0)
-      lav = Mem(la + start * sh.la_token)
-                .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
+      lav = Mem(la + start * sh.la_token).load<T>(lane < n ? la_at : kAbsent);
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
       const Head hd(sh, at, h);
-      xst[h].load(u + start * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+      xst[h].load(u + start * d.u_token + (int64_t)hd.h * P + hd.p0,
+                  typename XStage::In(d.u_token, hd.rows), n);
     }
-    bst.load(v + start * d.v_token, d.v_token, n, N);
+    bst.load(v + start * d.v_token, bin, n);
   };
   auto place = [&](int k) {
     if (sums_of >= 0) {
@@ -619,28 +645,36 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
       for (int t = 0; t < Tiles::kOwn; ++t) s[h][t] = f32x4{0, 0, 0, 0};
     }
   }
-  Stage<T, Q, PT, kThreads, VEC> xst[HB];
-  Stage<T, Q, NT, kThreads, VEC> bst, cst;
+  using XStage = Stage<T, Q, PT, kThreads, VEC>;
+  using NStage = Stage<T, Q, NT, kThreads, VEC>;
+  XStage xst[HB];
+  NStage bst, cst;
+  const typename NStage::In bin(d.v_token, N), cin(o.c_token, N);
   auto start = [&](int k) { return (int64_t)(first + k) * Q; };
   auto tokens = [&](int k) { return (int)min((int64_t)Q, (int64_t)sh.len - start(k)); };
-  auto fetch = [&](int k) {
-    const int n = tokens(k);
-    bst.load(v + start(k) * d.v_token, d.v_token, n, N);
-    cst.load(cc + start(k) * o.c_token, o.c_token, n, N);
+  // the next chunk's loads, in portions that do not hold the work up
+  auto fetch_b = [&](int k) {
+    if (k < count) bst.load(v + start(k) * d.v_token, bin, tokens(k));
+  };
+  auto fetch_c = [&](int k) {
+    if (k < count) cst.load(cc + start(k) * o.c_token, cin, tokens(k));
+  };
+  auto fetch_x = [&](int k) {
+    if (k >= count) return;
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
       const Head hd(sh, at, h);
-      xst[h].load(u + start(k) * d.u_token + (int64_t)hd.h * P + hd.p0, d.u_token, n, hd.rows);
+      xst[h].load(u + start(k) * d.u_token + (int64_t)hd.h * P + hd.p0,
+                  typename XStage::In(d.u_token, hd.rows), tokens(k));
     }
   };
   // Log decays come two chunks ahead from memory, their running sums one ahead
   // into LDS.
   float lav = 0.0f;
+  const uint32_t la_at = lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T);
   auto fetch_la = [&](int k) {
     if (k < count)
-      lav = Mem(la + start(k) * sh.la_token)
-                .load<T>(lane < tokens(k) ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T)
-                                          : kAbsent);
+      lav = Mem(la + start(k) * sh.la_token).load<T>(lane < tokens(k) ? la_at : kAbsent);
   };
   auto sums = [&](int k) {
     const Cum cum = cumulate(lav);
@@ -654,15 +688,17 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
       const Head hd(sh, at, h);
-      Stage<T, Q, PT, kThreads, VEC> y;
+      XStage y;
       y.take(xs[h], XS);
       y.put((T*)o.y + (((uint64_t)at.b * sh.len + start(k)) * sh.heads + hd.h) * P + hd.p0,
-            sh.heads * P, tokens(k), hd.rows);
+            typename XStage::In(sh.heads * P, hd.rows), tokens(k));
     }
   };
-  fetch(0);
+  if (sums_of >= 0) fetch_la(0);
+  fetch_b(0);
+  fetch_c(0);
+  fetch_x(0);
   if (sums_of >= 0) {
-    fetch_la(0);
     sums(0);
     fetch_la(1);
   }
@@ -687,11 +723,11 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
       }
     }
     __syncthreads();
-    if (k + 1 < count) fetch(k + 1);
     if (sums_of >= 0 && k + 1 < count) {
       sums(k + 1);
       fetch_la(k + 2);
     }
+    fetch_b(k + 1);
     {
       // rows r = 16 j + 4 g + i, column s = 16 wave + col
       Frag cf[NQ];
@@ -729,6 +765,7 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
         }
       }
     }
+    fetch_c(k + 1);
     Frag xf[HB][2];
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
@@ -768,6 +805,7 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
         acc[h][j] *= exp2_diff(hi[now][h][s16], lo[now][h][s16], 0.0f, 0.0f);
       }
     }
+    fetch_x(k + 1);
     update_state<T, NT, HB>(s, xf, bs, wt[now], total[now], t0);
     __syncthreads();
 #pragma unroll
@@ -842,27 +880,33 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   const uint64_t size = (uint64_t)P * N;
 
   {
-    Stage<T, Q, NT, 512, VEC> st;
-    st.load((const T*)a.b + b * a.b_batch + t0 * a.b_token + (int64_t)grp * N, a.b_token, n, N);
+    using NStage = Stage<T, Q, NT, 512, VEC>;
+    NStage st;
+    st.load((const T*)a.b + b * a.b_batch + t0 * a.b_token + (int64_t)grp * N,
+            typename NStage::In(a.b_token, N), n);
     st.store(bs, NS);
-    st.load((const T*)a.c + b * a.c_batch + t0 * a.c_token + (int64_t)grp * N, a.c_token, n, N);
+    st.load((const T*)a.c + b * a.c_batch + t0 * a.c_token + (int64_t)grp * N,
+            typename NStage::In(a.c_token, N), n);
     st.store(cs, NS);
   }
-  Stage<T, Q, PT, 512, VEC> xst, dyst;
-  Stage<T, PT, NT, 512, VEC> sst, rst;
+  using XStage = Stage<T, Q, PT, 512, VEC>;
+  using SStage = Stage<T, PT, NT, 512, VEC>;
+  XStage xst, dyst;
+  SStage sst, rst;
   float lav = 0.0f;
+  const uint32_t la_at =
+      lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent;
   auto fetch = [&](uint32_t k) {  // k: head of the split and channel tile
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
     const int p0 = pt * PT, rows = min(PT, P - p0);
-    lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h)
-              .load<T>(lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent);
-    xst.load((const T*)a.x + b * a.x_batch + t0 * a.x_token + (int64_t)h * P + p0, a.x_token, n,
-             rows);
-    dyst.load((const T*)a.dy + b * a.dy_batch + t0 * a.dy_token + (int64_t)h * P + p0, a.dy_token,
-              n, rows);
+    lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h).load<T>(la_at);
+    xst.load((const T*)a.x + b * a.x_batch + t0 * a.x_token + (int64_t)h * P + p0,
+             typename XStage::In(a.x_token, rows), n);
+    dyst.load((const T*)a.dy + b * a.dy_batch + t0 * a.dy_token + (int64_t)h * P + p0,
+              typename XStage::In(a.dy_token, rows), n);
     const uint64_t at = (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size + (uint64_t)p0 * N;
-    sst.load((const T*)a.s_in + at, N, rows, N);
-    rst.load((const T*)a.r_in + at, N, rows, N);
+    sst.load((const T*)a.s_in + at, typename SStage::In(N, N), rows);
+    rst.load((const T*)a.r_in + at, typename SStage::In(N, N), rows);
   };
   fetch(0);
   __syncthreads();

@@ -71,6 +71,10 @@ struct Rows {
 constexpr uint64_t kWholeTiles = 160;   // tiles that occupy most of 256 compute units
 constexpr uint64_t kPairGroups = 512;   // workgroups of pairs, two on each unit
 constexpr uint64_t kShortGroups = 256;  // workgroups of one tile
+// Up to this many segments each workgroup adds up the summaries before its own
+// (segs / 2 states read on average); more go through the join kernel (each read
+// and written once, a launch more).
+constexpr uint32_t kJoinedSegs = 12;
 ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   ScanShape s{};
   s.batch = d->batch;
@@ -97,6 +101,7 @@ ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   }
   s.seg_chunks = (uint32_t)((s.chunks + segs - 1) / segs);
   s.segs = s.chunks ? (s.chunks + s.seg_chunks - 1) / s.seg_chunks : 1;
+  s.joined = s.segs > kJoinedSegs;
   return s;
 }
 

@@ -34,6 +34,7 @@ struct ScanShape {
   uint32_t chunks;      // ceil(len / kChunk)
   uint32_t seg_chunks;  // chunks per segment
   uint32_t segs;
+  bool joined;          // the summaries of many segments are joined by a kernel of its own
   uint32_t ptiles;      // ceil(head_dim / kPTile)
   uint32_t tiles;       // channel tiles in one workgroup: 1, or 2 (aligned bfloat16)
   const void* la;

@@ -19,13 +19,19 @@ namespace fesc {
 
 namespace {
 
-constexpr int kUnit = 8;       // neighbouring channels of one lane
+constexpr int kUnit = 8;       // channels of one lane's unit
 constexpr int kThreads = 256;
 
-// Eight neighbouring channels as they lie in memory; those at or past `left`
-// are zero.  VEC: rows start at multiples of 16 bytes and hold whole units.
-template <typename T, bool VEC>
+// Eight channels as they lie in memory.  VEC (rows start at multiples of 16
+// bytes and hold whole units): neighbours.  Otherwise STEP apart, so that the
+// lanes of a wave read neighbours.  Those at or past `left` are zero.
+template <typename T, bool VEC, int LANES>
 struct Unit {
+  static constexpr int STEP = VEC ? 1 : LANES;
+  // first channel of unit j of a lane
+  __device__ __forceinline__ static int channel(int lane, int j) {
+    return VEC ? (lane + j * LANES) * kUnit : lane + j * LANES * kUnit;
+  }
   static constexpr int kWords = kUnit * sizeof(T) / 4;
   uint32_t w[kWords];
 
@@ -43,7 +49,7 @@ struct Unit {
       for (int i = 0; i < kWords; ++i) w[i] = 0;
 #pragma unroll
       for (int i = 0; i < kUnit; ++i) {
-        const uint32_t v = m.load_bits<T>(i < left ? at + i * (uint32_t)sizeof(T) : kAbsent);
+        const uint32_t v = m.load_bits<T>(i * STEP < left ? at + i * STEP * (uint32_t)sizeof(T) : kAbsent);
         if constexpr (sizeof(T) == 4)
           w[i] = v;
         else
@@ -77,7 +83,7 @@ struct Unit {
     } else {
 #pragma unroll
       for (int i = 0; i < kUnit; ++i)
-        m.store_bits<T>(i < left ? at + i * (uint32_t)sizeof(T) : kAbsent,
+        m.store_bits<T>(i * STEP < left ? at + i * STEP * (uint32_t)sizeof(T) : kAbsent,
                         sizeof(T) == 4 ? w[i] : w[i / 2] >> (16 * (i & 1)) & 0xffffu);
     }
   }
@@ -129,11 +135,11 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
   __shared__ float2 red[kThreads / 64];
   constexpr int kRows = kThreads / TPR;
   const int lane = threadIdx.x % TPR;
-  Unit<T, VEC> kk[UPT], ww[UPT];
+  Unit<T, VEC, TPR> kk[UPT], ww[UPT];
   const Mem km(a.k), wm(a.w);
 #pragma unroll
   for (int j = 0; j < UPT; ++j) {
-    const int e = (lane + j * TPR) * kUnit, left = (int)a.width - e;
+    const int e = Unit<T, VEC, TPR>::channel(lane, j), left = (int)a.width - e;
     kk[j].load(km, e, left);
     ww[j].load(wm, e, left);
   }
@@ -143,10 +149,10 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
     const int width = row < a.rows ? a.width : 0;  // of an absent row: nothing
     const Mem ma((const T*)a.a + row * a.a_row), mb((const T*)a.b + row * a.b_row);
     const Mem mc((const T*)a.c + row * a.c_row);
-    Unit<T, VEC> ua[UPT], ub[UPT], uc[UPT];
+    Unit<T, VEC, TPR> ua[UPT], ub[UPT], uc[UPT];
 #pragma unroll
     for (int j = 0; j < UPT; ++j) {
-      const int e = (lane + j * TPR) * kUnit, left = width - e;
+      const int e = Unit<T, VEC, TPR>::channel(lane, j), left = width - e;
       ua[j].load(ma, e, left);
       ub[j].load(mb, e, left);
       if constexpr (GATED) uc[j].load(mc, e, left);
@@ -171,8 +177,8 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
     const Mem mu((T*)a.u + row * a.width), mr((T*)a.r_new + row * a.width);
 #pragma unroll
     for (int j = 0; j < UPT; ++j) {
-      const int e = (lane + j * TPR) * kUnit, left = width - e;
-      Unit<T, VEC> o;
+      const int e = Unit<T, VEC, TPR>::channel(lane, j), left = width - e;
+      Unit<T, VEC, TPR> o;
       if constexpr (!GATED) {
 #pragma unroll
         for (int i = 0; i < kUnit; i += 4)
@@ -210,19 +216,19 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(NormArgs a) {
   __shared__ Sums red[kThreads / 64];
   __shared__ float part[kRows > 1 ? 2 * W : 1];
   const int lane = threadIdx.x % TPR;
-  Unit<T, VEC> kk[UPT], ww[UPT];
+  Unit<T, VEC, TPR> kk[UPT], ww[UPT];
   float dk[UPT][kUnit], dw[UPT][kUnit];
   const Mem km(a.k), wm(a.w);
 #pragma unroll
   for (int j = 0; j < UPT; ++j) {
-    const int e = (lane + j * TPR) * kUnit, left = (int)a.width - e;
+    const int e = Unit<T, VEC, TPR>::channel(lane, j), left = (int)a.width - e;
     kk[j].load(km, e, left);
     ww[j].load(wm, e, left);
 #pragma unroll
     for (int i = 0; i < kUnit; ++i) dk[j][i] = dw[j][i] = 0.0f;
   }
   struct Row {
-    Unit<T, VEC> a[UPT], b[UPT], c[UPT], du[UPT], dr[UPT];
+    Unit<T, VEC, TPR> a[UPT], b[UPT], c[UPT], du[UPT], dr[UPT];
   };
   auto fetch = [&](Row& r, uint64_t base) {
     const uint64_t row = base + own_row<TPR>();
@@ -232,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(NormArgs a) {
     const Mem mr((const T*)a.dr_new + row * a.dr_row);
 #pragma unroll
     for (int j = 0; j < UPT; ++j) {
-      const int e = (lane + j * TPR) * kUnit, left = width - e;
+      const int e = Unit<T, VEC, TPR>::channel(lane, j), left = width - e;
       r.a[j].load(ma, e, left);
       r.b[j].load(mb, e, left);
       if constexpr (GATED) r.c[j].load(mc, e, left);
@@ -283,8 +289,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(NormArgs a) {
     const Mem mc((T*)a.dc + row * a.width);
 #pragma unroll
     for (int j = 0; j < UPT; ++j) {
-      const int e = (lane + j * TPR) * kUnit, left = width - e;
-      Unit<T, VEC> o1, o2, o3;
+      const int e = Unit<T, VEC, TPR>::channel(lane, j), left = width - e;
+      Unit<T, VEC, TPR> o1, o2, o3;
 #pragma unroll
       for (int i4 = 0; i4 < kUnit; i4 += 4) {
         f32x4 v1, v2, v3;
@@ -334,7 +340,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(NormArgs a) {
         for (int j = 0; j < UPT; ++j) {
 #pragma unroll
           for (int i = 0; i < kUnit; ++i) {
-            const int e = (lane + j * TPR) * kUnit + i;
+            const int e = Unit<T, VEC, TPR>::channel(lane, j) + i * Unit<T, VEC, TPR>::STEP;
             part[e] = (w ? part[e] : 0.0f) + dk[j][i];
             part[W + e] = (w ? part[W + e] : 0.0f) + dw[j][i];
           }
@@ -351,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(NormArgs a) {
     for (int j = 0; j < UPT; ++j) {
 #pragma unroll
       for (int i = 0; i < kUnit; ++i) {
-        const int e = (lane + j * TPR) * kUnit + i;
+        const int e = Unit<T, VEC, TPR>::channel(lane, j) + i * Unit<T, VEC, TPR>::STEP;
         if (e < (int)a.width) {
           out[e] = dk[j][i];
           out[a.width + e] = dw[j][i];

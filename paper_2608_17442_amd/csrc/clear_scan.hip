@@ -239,22 +239,19 @@ struct Stage {
       }
     }
   }
-  // sum of the products of these values with those at the same places of a tile
-  __device__ __forceinline__ float dot(const T* tile, int pitch) const {
+  // sum of the products of these values with those at the same places of `o`
+  __device__ __forceinline__ float dot(const Stage& o) const {
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-      const int i = threadIdx.x + k * THREADS;
-      const u32x4 o =
-          *reinterpret_cast<const u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
+        const uint32_t v = r[k][j], w = o.r[k][j];
         if constexpr (sizeof(T) == 4) {
-          s = __builtin_fmaf(__uint_as_float(r[k][j]), __uint_as_float(o[j]), s);
+          s = __builtin_fmaf(__uint_as_float(v), __uint_as_float(w), s);
         } else {
-          s = __builtin_fmaf(__uint_as_float(r[k][j] << 16), __uint_as_float(o[j] << 16), s);
-          s = __builtin_fmaf(__uint_as_float(r[k][j] & 0xffff0000u),
-                             __uint_as_float(o[j] & 0xffff0000u), s);
+          s = __builtin_fmaf(__uint_as_float(v << 16), __uint_as_float(w << 16), s);
+          s = __builtin_fmaf(__uint_as_float(v & 0xffff0000u), __uint_as_float(w & 0xffff0000u), s);
         }
       }
     }
@@ -384,6 +381,36 @@ __device__ __forceinline__ void load_state(f32x4 (&s)[NTILES], const float* base
     s[t] = m.load_four<VEC>((p * N + n) * 4, p < rows ? N - n : 0);
   }
 }
+// The state that enters segment `seg` of a head.  Joined: as k_scan_join left it.
+// Otherwise from the summaries of the segments before, the summary of segment j
+// lying in the place of segment j + 1.
+template <bool VEC, int NTILES>
+__device__ __forceinline__ void enter_segment(f32x4 (&s)[NTILES], const ScanShape& sh,
+                                              const ScanDir& d, uint64_t head, uint32_t seg,
+                                              int p0, int p, int rows, int t0) {
+  const int N = sh.d_state;
+  const uint64_t size = (uint64_t)sh.head_dim * N, tile = (uint64_t)p0 * N;
+  const float* from = d.init ? d.init + head * size : nullptr;
+  const float* segs = d.seg_states ? d.seg_states + head * sh.segs * size : nullptr;
+  if (sh.joined && segs) from = segs + seg * size;
+  if (from) {
+    load_state<VEC>(s, from + tile, p, rows, N, t0);
+  } else {
+#pragma unroll
+    for (int t = 0; t < NTILES; ++t) s[t] = f32x4{0, 0, 0, 0};
+  }
+  if (sh.joined || !segs) return;
+  for (uint32_t j = 1; j <= seg; ++j) {
+    f32x4 own[NTILES];
+    load_state<VEC>(own, segs + j * size + tile, p, rows, N, t0);
+    const float decay = d.seg_decay[head * sh.segs + j - 1];
+#pragma unroll
+    for (int t = 0; t < NTILES; ++t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(decay, s[t][i], own[t][i]);
+    }
+  }
+}
 template <bool VEC, typename T, int NTILES>
 __device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], T* base, int p, int rows,
                                             int N, int t0) {
@@ -496,15 +523,11 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
 #pragma unroll
   for (int h = 0; h < HB; ++h) {
     const Head hd(sh, at, h);
-    const float* from = summaries      ? nullptr
-                        : d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
-                        : d.init       ? d.init + hd.at * size
-                                       : nullptr;
-    if (from) {
-      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
-    } else {
+    if (summaries) {
 #pragma unroll
       for (int t = 0; t < Tiles::kOwn; ++t) s[h][t] = f32x4{0, 0, 0, 0};
+    } else {
+      enter_segment<VEC>(s[h], sh, d, hd.at, at.seg, hd.p0, p, hd.rows, t0);
     }
   }
   using XStage = Stage<T, Q, PT, kThreads, VEC>;
@@ -635,15 +658,7 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
 #pragma unroll
   for (int h = 0; h < HB; ++h) {
     const Head hd(sh, at, h);
-    const float* from = d.seg_states ? d.seg_states + (hd.at * sh.segs + at.seg) * size
-                        : d.init     ? d.init + hd.at * size
-                                     : nullptr;
-    if (from) {
-      load_state<VEC>(s[h], from + (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
-    } else {
-#pragma unroll
-      for (int t = 0; t < Tiles::kOwn; ++t) s[h][t] = f32x4{0, 0, 0, 0};
-    }
+    enter_segment<VEC>(s[h], sh, d, hd.at, at.seg, hd.p0, p, hd.rows, t0);
   }
   using XStage = Stage<T, Q, PT, kThreads, VEC>;
   using NStage = Stage<T, Q, NT, kThreads, VEC>;
@@ -862,7 +877,9 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   __shared__ __align__(16) T dys[Q * XS];
   __shared__ __align__(16) T sr[PT * NS];
   __shared__ __align__(16) float hi[Q], lo[Q], ec[Q], wt[Q];
-  __shared__ float us[Q], vs[Q], colsum[Q], rowsum[4][Q], dots[8];
+  // of the head at hand and of the one before, whose dla is still to be formed
+  __shared__ float us[2][Q], vs[2][Q], colsum[2][Q], rowsum[2][4][Q], dots[2][8], total[2];
+  __shared__ bool reset[2][Q];
   using Frag = typename Elem<T>::Frag;
   using Four = typename Elem<T>::Four;
   const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
@@ -896,7 +913,9 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   float lav = 0.0f;
   const uint32_t la_at =
       lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent;
-  auto fetch = [&](uint32_t k) {  // k: head of the split and channel tile
+  // the loads of round k (head of the split and channel tile), in portions that
+  // do not hold the work up
+  auto fetch_tokens = [&](uint32_t k) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
     const int p0 = pt * PT, rows = min(PT, P - p0);
     lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h).load<T>(la_at);
@@ -904,11 +923,21 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
              typename XStage::In(a.x_token, rows), n);
     dyst.load((const T*)a.dy + b * a.dy_batch + t0 * a.dy_token + (int64_t)h * P + p0,
               typename XStage::In(a.dy_token, rows), n);
-    const uint64_t at = (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size + (uint64_t)p0 * N;
-    sst.load((const T*)a.s_in + at, typename SStage::In(N, N), rows);
-    rst.load((const T*)a.r_in + at, typename SStage::In(N, N), rows);
   };
-  fetch(0);
+  auto state_at = [&](uint32_t k) {
+    const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
+    return (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size + (uint64_t)pt * PT * N;
+  };
+  auto state_rows = [&](uint32_t k) { return min(PT, P - (int)(k % sh.ptiles) * PT); };
+  auto fetch_state = [&](uint32_t k) {
+    sst.load((const T*)a.s_in + state_at(k), typename SStage::In(N, N), state_rows(k));
+  };
+  auto fetch_adjoint = [&](uint32_t k) {
+    rst.load((const T*)a.r_in + state_at(k), typename SStage::In(N, N), state_rows(k));
+  };
+  fetch_tokens(0);
+  fetch_state(0);
+  fetch_adjoint(0);
   __syncthreads();
 
   // waves 0..3: tiles (s = 16 j + 4 g + i, r = 16 tile + col) of G and W;
@@ -930,25 +959,60 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
       }
     }
   }
-  float dla = 0.0f;  // wave 0: token `lane`, summed over the channel tiles of a head
+  // dla of round k, by one wave, from what the waves left in LDS
+  float dla = 0.0f;  // token `lane`, summed over the channel tiles of a head
+  auto finish = [&](uint32_t k) {
+    const int b2 = k & 1;
+    float base = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) base += dots[b2][x];
+    const float u = us[b2][lane] +
+                    ((rowsum[b2][0][lane] + rowsum[b2][1][lane]) +
+                     (rowsum[b2][2][lane] + rowsum[b2][3][lane])) -
+                    colsum[b2][lane];
+    const float v = vs[b2][lane];
+    float after = u, before = v;  // sums from the token on, and up to it
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+      const float p = __shfl_down(after, x), q = __shfl_up(before, x);
+      after += lane + x < 64 ? p : 0.0f;
+      before += lane >= x ? q : 0.0f;
+    }
+    const float upto = __shfl_up(before, 1);
+    // before a reset nothing counts: the exact zero, not the sums' remainder
+    dla += reset[b2][lane] ? 0.0f : after + (lane ? upto : 0.0f) + base * total[b2];
+    if (k % sh.ptiles + 1 == sh.ptiles) {
+      const uint32_t h = grp * per_group + h0 + k / sh.ptiles;
+      if (lane < n) ((T*)a.dla)[((uint64_t)b * sh.len + t0 + lane) * sh.heads + h] = (T)dla;
+      dla = 0.0f;
+    }
+  };
+  // The wave with least of K forms dla of the round before, and the one whose
+  // loads are done first the running sums of the next.
+  constexpr int kFinish = 3, kSums = 0;
+  Cum cum;
+  if (wave == kSums) cum = cumulate(lav);
   const uint32_t rounds = hn * sh.ptiles;
   for (uint32_t k = 0; k < rounds; ++k) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
-    const int p0 = pt * PT, rows = min(PT, P - p0);
-    Cum cum;
-    if (wave == 0) cum = cumulate(lav);
-    const bool reset = lav < kReset;
+    const int p0 = pt * PT, rows = min(PT, P - p0), now = k & 1;
     __syncthreads();
     xst.store(xs, XS);
     dyst.store(dys, XS);
     sst.store(sr, NS);
-    if (wave == 0) {
+    if (wave == kSums) {
       hi[lane] = cum.hi;
       lo[lane] = cum.lo;
       ec[lane] = cum.e;
       wt[lane] = cum.w;
+      reset[now][lane] = lav < kReset;
+      if (lane == 0) total[now] = cum.total;
     }
+    const float dot = sum_groups(sum16(rst.dot(sst)));
+    if (lane == 0) dots[now][wave] = dot;
     __syncthreads();
+    if (k + 1 < rounds) fetch_tokens(k + 1);
+    if (wave == kFinish && k) finish(k - 1);
     Four dg[4];  // D G as an operand, summed over s
     if (left) {
       const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
@@ -977,11 +1041,11 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float s = sum16(m[i]);
-          if (col == 0) rowsum[tile][16 * j + 4 * g + i] = s;
+          if (col == 0) rowsum[now][tile][16 * j + 4 * g + i] = s;
         }
       }
       cols = sum_groups(cols);
-      if (g == 0) colsum[16 * tile + col] = cols;
+      if (g == 0) colsum[now][16 * tile + col] = cols;
     } else {
       const float es = ec[16 * tile + col];
       float sum = 0.0f;
@@ -999,14 +1063,13 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
         sum += (acc[0] * cv[0] + acc[1] * cv[1]) + (acc[2] * cv[2] + acc[3] * cv[3]);
       }
       sum = sum_groups(sum);
-      if (g == 0) us[16 * tile + col] = sum;
+      if (g == 0) us[now][16 * tile + col] = sum;
     }
-    const float dot = sum_groups(sum16(rst.dot(sr, NS)));
-    if (lane == 0) dots[wave] = dot;
+    if (k + 1 < rounds) fetch_state(k + 1);
     __syncthreads();
     rst.store(sr, NS);
     __syncthreads();
-    if (k + 1 < rounds) fetch(k + 1);
+    if (k + 1 < rounds) fetch_adjoint(k + 1);
     if (left) {
       const float wr = wt[16 * tile + col];
       Frag bf[NT / 32];
@@ -1051,34 +1114,12 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
         sum += (acc[0] * bv[0] + acc[1] * bv[1]) + (acc[2] * bv[2] + acc[3] * bv[3]);
       }
       sum = sum_groups(sum);
-      if (g == 0) vs[16 * tile + col] = sum;
+      if (g == 0) vs[now][16 * tile + col] = sum;
     }
-    __syncthreads();
-    if (wave == 0) {
-      float base = 0.0f;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) base += dots[x];
-      const float u = us[lane] +
-                      ((rowsum[0][lane] + rowsum[1][lane]) + (rowsum[2][lane] + rowsum[3][lane])) -
-                      colsum[lane];
-      const float v = vs[lane];
-      float after = u, before = v;  // sums from the token on, and up to it
-#pragma unroll
-      for (int x = 1; x < 64; x *= 2) {
-        const float p = __shfl_down(after, x), q = __shfl_up(before, x);
-        after += lane + x < 64 ? p : 0.0f;
-        before += lane >= x ? q : 0.0f;
-      }
-      const float upto = __shfl_up(before, 1);
-      // before a reset nothing counts: the exact zero, not the sums' remainder
-      dla += reset ? 0.0f : after + (lane ? upto : 0.0f) + base * cum.total;
-      if (pt + 1 == sh.ptiles) {
-        if (lane < n)
-          ((T*)a.dla)[((uint64_t)b * sh.len + t0 + lane) * sh.heads + h] = (T)dla;
-        dla = 0.0f;
-      }
-    }
+    if (wave == kSums && k + 1 < rounds) cum = cumulate(lav);
   }
+  __syncthreads();
+  if (wave == kFinish) finish(rounds - 1);
   // W to LDS (rows s, columns r), then its products with B and C
   if (left) {
 #pragma unroll
@@ -1190,9 +1231,11 @@ hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipS
   if (sh.segs > 1) {
     k_scan_states<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
-    const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
-    k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
-    if (hipError_t e = hipGetLastError()) return e;
+    if (sh.joined) {
+      const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
+      k_scan_join<<<dim3(blocks * sh.batch * sh.heads, 1, nd), 256, 0, s>>>(sh, d0, d1);
+      if (hipError_t e = hipGetLastError()) return e;
+    }
   }
   if (!main) return hipSuccess;
   k_scan_states<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, false);

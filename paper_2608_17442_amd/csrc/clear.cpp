@@ -74,7 +74,7 @@ constexpr uint64_t kShortGroups = 256;  // workgroups of one tile
 // Up to this many segments each workgroup adds up the summaries before its own
 // (segs / 2 states read on average); more go through the join kernel (each read
 // and written once, a launch more).
-constexpr uint32_t kJoinedSegs = 12;
+constexpr uint32_t kJoinedSegs = 5;
 ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   ScanShape s{};
   s.batch = d->batch;

@@ -400,14 +400,23 @@ __device__ __forceinline__ void enter_segment(f32x4 (&s)[NTILES], const ScanShap
     for (int t = 0; t < NTILES; ++t) s[t] = f32x4{0, 0, 0, 0};
   }
   if (sh.joined || !segs) return;
-  for (uint32_t j = 1; j <= seg; ++j) {
-    f32x4 own[NTILES];
-    load_state<VEC>(own, segs + j * size + tile, p, rows, N, t0);
-    const float decay = d.seg_decay[head * sh.segs + j - 1];
+  constexpr int kAtOnce = NTILES <= 4 ? 4 : 2;  // loads under way
+  for (uint32_t j0 = 1; j0 <= seg; j0 += kAtOnce) {
+    f32x4 own[kAtOnce][NTILES];
+    float decay[kAtOnce];
 #pragma unroll
-    for (int t = 0; t < NTILES; ++t) {
+    for (int k = 0; k < kAtOnce; ++k) {  // past the last: nothing, kept as it is
+      const uint32_t j = min(j0 + k, seg);
+      load_state<VEC>(own[k], segs + j * size + tile, p, j0 + k <= seg ? rows : 0, N, t0);
+      decay[k] = j0 + k <= seg ? d.seg_decay[head * sh.segs + j - 1] : 1.0f;
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(decay, s[t][i], own[t][i]);
+    for (int k = 0; k < kAtOnce; ++k) {
+#pragma unroll
+      for (int t = 0; t < NTILES; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(decay[k], s[t][i], own[k][t][i]);
+      }
     }
   }
 }

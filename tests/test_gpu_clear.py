@@ -544,3 +544,27 @@ def test_refusals(clear):
         with pytest.raises(error):
             call()
             pytest.fail(f"call {k} was not refused")
+
+
+# -------------------------------------------------------------------- example
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_example_learns_and_serves(clear, dtype):
+    """The example's block: its loss falls by half, and token by token it gives
+    what it gives at once, to the roundings on the way: four on either side
+    between the recurrence and the output, each of at most one unit (bfloat16:
+    2^-8; float32, whose sums have some hundreds of terms: 2^-16), on values up
+    to some five times the root mean square."""
+    step(f"example {dtype}")
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "clear_block.py")
+    spec = importlib.util.spec_from_file_location("clear_block", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    block = example.Block(dtype=dtype)
+    first, last = example.train(block, 40, 4, 200)
+    assert last < 0.5 * first
+    unit = 2.0 ** (-8 if dtype == BF16 else -16)
+    assert example.serve(block, 5, 100, 10) <= 2 * 4 * 5 * unit

@@ -257,6 +257,7 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
               .len(d->d_state).apart(d->x_token, d->head_dim).apart(d->b_token, d->d_state)
               .apart(d->c_token, d->d_state).ok;
   if (!s.vec) s.tiles = 1;
+  s.exact = hT != nullptr;
   dir.u = x;
   dir.v = B;
   dir.u_token = d->x_token;
@@ -294,6 +295,7 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
               .apart(d->x_token, d->head_dim).apart(d->b_token, d->d_state)
               .apart(d->c_token, d->d_state).apart(d->dy_token, d->head_dim).ok;
   if (!s.vec) s.tiles = 1;
+  s.exact = dh0 != nullptr;
   dir[0].u = x;
   dir[0].v = B;
   dir[0].u_token = d->x_token;

@@ -39,7 +39,8 @@ struct ScanShape {
   uint32_t tiles;       // channel tiles in one workgroup: 1, or 2 (aligned bfloat16)
   const void* la;
   int64_t la_token, la_batch;
-  bool vec;  // every row of every array starts at a multiple of 16 bytes
+  bool vec;    // every row of every array starts at a multiple of 16 bytes
+  bool exact;  // a state is an output
 };
 
 struct ScanOut {  // outputs of a forward scan beside the final state

@@ -12,8 +12,9 @@
 // stays in registers, in fp32, from chunk to chunk.  Products with the state
 // and with the matrix of decays take these operands rounded to the call's
 // type (one rounding on each path to an output, as large as that of the
-// output itself); the state's own update does not round: the weighted inputs
-// enter as three bf16 parts that sum to the fp32 value exactly.
+// output itself); the state's own update does not add to that: the weighted
+// inputs enter as bf16 parts, three that sum to the fp32 value exactly where the
+// state (or its gradient) is an output of the call, otherwise two.
 #include "clear.hpp"
 #include "clear_mem.hpp"
 #include "fesc_internal.hpp"
@@ -109,36 +110,39 @@ __device__ __forceinline__ f32x8 join(const f32x4& a, const f32x4& b) {
 __device__ __forceinline__ f32x4 widen(const bf16x4& v) { return __builtin_convertvector(v, f32x4); }
 __device__ __forceinline__ f32x4 widen(const f32x4& v) { return v; }
 
-// The parts of a fp32 operand in the call's type: itself, or three bf16
-// values (each the leading 8 bits of what the ones before leave) whose sum it
-// is.
-template <typename T>
+// The parts of a fp32 operand in the call's type: itself, or COUNT bf16 values.
+// Three, each the leading 8 bits of what the ones before leave, sum to it
+// exactly; two, each rounded to nearest, to within 2^-17 of it.
+template <typename T, int COUNT>
 struct Parts;
-template <>
-struct Parts<float> {
+template <int COUNT>
+struct Parts<float, COUNT> {
   static constexpr int kCount = 1;
   f32x8 p[1];
   __device__ __forceinline__ void split(const f32x4& a, const f32x4& b) { p[0] = join(a, b); }
 };
-template <>
-struct Parts<__bf16> {
-  static constexpr int kCount = 3;
-  bf16x8 p[3];
+template <int COUNT>
+struct Parts<__bf16, COUNT> {
+  static constexpr int kCount = COUNT;
+  bf16x8 p[COUNT];
   __device__ __forceinline__ void split(const f32x4& a, const f32x4& b) {
     f32x8 v = join(a, b);
+    if constexpr (COUNT == 2) {
+      p[0] = __builtin_convertvector(v, bf16x8);
+      p[1] = __builtin_convertvector(v - __builtin_convertvector(p[0], f32x8), bf16x8);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      u32x4 w;
+      for (int k = 0; k < 3; ++k) {
+        u32x4 w;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        w[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]),
-                                     0x07060302u);
-      p[k] = __builtin_bit_cast(bf16x8, w);
-      if (k < 2) {
+        for (int j = 0; j < 4; ++j)
+          w[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]),
+                                       0x07060302u);
+        p[k] = __builtin_bit_cast(bf16x8, w);
+        if (k < 2) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-          v[j] = v[j] - hi;
+          for (int j = 0; j < 8; ++j)
+            v[j] -= __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
         }
       }
     }
@@ -460,7 +464,7 @@ __device__ __forceinline__ f32x4 half(const f32x8& v, int k) {
 // S' = total S + sum_r w_r x_r B_r^T over the chunk in LDS; xf: this wave's rows
 // of x as operands.  Two state tiles at a time, whose products do not wait for
 // each other's sums.
-template <typename T, int NT, int HB, int OWN>
+template <typename T, int NT, int PARTS, int HB, int OWN>
 __device__ __forceinline__ void update_state(f32x4 (&s)[HB][OWN],
                                              const typename Elem<T>::Frag (&xf)[HB][2],
                                              const T* bs, const float (&w)[HB][Q],
@@ -476,7 +480,7 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[HB][OWN],
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int r = 32 * q + 4 * g;
-    Parts<T> x[HB];
+    Parts<T, PARTS> x[HB];
 #pragma unroll
     for (int h = 0; h < HB; ++h)
       x[h].split(half(xf[h][q], 0) * *reinterpret_cast<const f32x4*>(w[h] + r),
@@ -488,7 +492,7 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[HB][OWN],
       for (int f = 0; f < 2; ++f)
         b[f] = join(state_four(bs, NS, r, t0 + t + f), state_four(bs, NS, r + 16, t0 + t + f));
 #pragma unroll
-      for (int k = 0; k < Parts<T>::kCount; ++k) {
+      for (int k = 0; k < Parts<T, PARTS>::kCount; ++k) {
 #pragma unroll
         for (int h = 0; h < HB; ++h) {
 #pragma unroll
@@ -503,7 +507,7 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[HB][OWN],
 // zero, and its total decay, to seg_states and seg_decay.  Otherwise from the
 // state that enters the segment: the states that enter the chunks, and the
 // final state.  Chunks lie in LDS in turn in two places: one barrier each.
-template <typename T, int NT, bool VEC, int HB, int EW>
+template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
 __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_scan_states(
     ScanShape sh, ScanDir d0, ScanDir d1, bool summaries) {
   using Tiles = ScanTiles<T, NT, HB, EW>;
@@ -593,7 +597,7 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
       for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[k & 1][h], XS, q, 16 * wave);
       decay[h] *= total[k & 1][h];
     }
-    update_state<T, NT, HB>(s, xf, bs[k & 1], wt[k & 1], total[k & 1], t0);
+    update_state<T, NT, PARTS, HB>(s, xf, bs[k & 1], wt[k & 1], total[k & 1], t0);
     if (k + 1 < count) place(k + 1);
   }
 #pragma unroll
@@ -634,7 +638,7 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
 // EW = 2), and writes their products with each tile's decays to LDS; meanwhile the
 // state's part of y^T for its 16 channels and all tokens (half e), and its part
 // of the new state; then the chunk's own part of y^T from what all waves wrote.
-template <typename T, int NT, bool VEC, int HB, int EW>
+template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
 __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_scan_out(
     ScanShape sh, ScanDir d, ScanOut o) {
   using Tiles = ScanTiles<T, NT, HB, EW>;
@@ -830,7 +834,7 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
       }
     }
     fetch_x(k + 1);
-    update_state<T, NT, HB>(s, xf, bs, wt[now], total[now], t0);
+    update_state<T, NT, PARTS, HB>(s, xf, bs, wt[now], total[now], t0);
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -1233,12 +1237,12 @@ __global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to
   if (i < count) to[i] = from ? from[i] : 0.0f;
 }
 
-template <typename T, int NT, bool VEC, int HB, int EW>
+template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
   const ScanDir &d0 = d[0], &d1 = d[nd - 1];
   const dim3 grid(sh.batch * sh.segs * (sh.heads * sh.ptiles / HB), 1, nd);
   if (sh.segs > 1) {
-    k_scan_states<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, true);
+    k_scan_states<T, NT, VEC, PARTS, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
     if (sh.joined) {
       const uint32_t blocks = (sh.head_dim * sh.d_state + 255) / 256;
@@ -1247,27 +1251,35 @@ hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipS
     }
   }
   if (!main) return hipSuccess;
-  k_scan_states<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, false);
+  k_scan_states<T, NT, VEC, PARTS, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, false);
   return hipGetLastError();
 }
-template <typename T, int NT, bool VEC, int HB, int EW>
+template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
 hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
-  if (hipError_t e = states<T, NT, VEC, HB, EW>(sh, &d, 1, false, s)) return e;
+  if (hipError_t e = states<T, NT, VEC, PARTS, HB, EW>(sh, &d, 1, false, s)) return e;
   const uint32_t grid = sh.batch * sh.segs * (sh.heads * sh.ptiles / HB);
-  k_scan_out<T, NT, VEC, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d, o);
+  k_scan_out<T, NT, VEC, PARTS, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d, o);
   return hipGetLastError();
 }
+// The forms of a call: see ScanTiles and Parts.  Calls on unaligned rows and in
+// float32 take the one that is kept for them.
+#define FESC_SCAN_FORMS(CALL)                                  \
+  if constexpr (sizeof(T) == 2 && VEC) {                       \
+    if (sh.exact) return sh.tiles == 2 ? CALL(3, 2, 1) : CALL(3, 1, 2); \
+    return sh.tiles == 2 ? CALL(2, 2, 1) : CALL(2, 1, 2);      \
+  }                                                            \
+  return CALL(3, 1, 2)
 template <typename T, int NT, bool VEC>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, hipStream_t s) {
-  if constexpr (sizeof(T) == 2 && VEC)
-    if (sh.tiles == 2) return states<T, NT, VEC, 2, 1>(sh, d, nd, true, s);
-  return states<T, NT, VEC, 1, 2>(sh, d, nd, true, s);
+#define FORM(PARTS, HB, EW) (states<T, NT, VEC, PARTS, HB, EW>(sh, d, nd, true, s))
+  FESC_SCAN_FORMS(FORM);
+#undef FORM
 }
 template <typename T, int NT, bool VEC>
 hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
-  if constexpr (sizeof(T) == 2 && VEC)
-    if (sh.tiles == 2) return outputs<T, NT, VEC, 2, 1>(sh, d, o, s);
-  return outputs<T, NT, VEC, 1, 2>(sh, d, o, s);
+#define FORM(PARTS, HB, EW) (outputs<T, NT, VEC, PARTS, HB, EW>(sh, d, o, s))
+  FESC_SCAN_FORMS(FORM);
+#undef FORM
 }
 
 // One instance per element type, padded state size and alignment.

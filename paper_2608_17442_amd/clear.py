@@ -182,12 +182,13 @@ def _scan_plan(x, la, B, C, h0, dy=None):
     G, N = B.shape[2:]
     if h0 is not None:
         _state(h0, (b, H, P, N), "h0", x)
+    # without dy: the strides of a contiguous one
     d = _ScanDesc(_TYPES[x.dtype], b, n, H, P, G, N, x.stride(1), x.stride(0), la.stride(1),
                   la.stride(0), B.stride(1), B.stride(0), C.stride(1), C.stride(0),
-                  dy.stride(1) if dy is not None else 0, dy.stride(0) if dy is not None else 0)
+                  *((H * P, n * H * P) if dy is None else (dy.stride(1), dy.stride(0))))
     plan = _Plan(d, x.device)
     plan.space = _space(_lib.fesc_clear_scan_workspace, plan.ref, 0)
-    plan.grad_space = _space(_lib.fesc_clear_scan_workspace, plan.ref, 1) if dy is not None else 0
+    plan.grad_space = _space(_lib.fesc_clear_scan_workspace, plan.ref, 1)
     plan.shapes = (tuple(x.shape), (b, H, P, N))
     return plan
 
@@ -207,6 +208,7 @@ class _Scan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, la, B, C, h0, want_state, plan):
         ctx.set_materialize_grads(False)
+        ctx.plan = plan
         ctx.save_for_backward(x, la, B, C, h0)
         y, h = _scan_forward(plan, x, la, B, C, h0, want_state)
         return (y, h) if want_state else y
@@ -223,13 +225,11 @@ class _Scan(torch.autograd.Function):
             dy = dy.contiguous()
         if dh is not None:
             dh = dh.contiguous()
-        plan = _plan(_key("scan gradient", x, la, B, C, h0, dy), _scan_plan, (x, la, B, C, h0, dy))
-
-        def like(t):
-            return torch.empty(t.shape, dtype=t.dtype, device=plan.device)
-
-        dx, dla, db, dc = like(x), like(la), like(B), like(C)
-        dh0 = like(h0) if h0 is not None and ctx.needs_input_grad[4] else None
+        plan = ctx.plan if dy.is_contiguous() else _plan(
+            _key("scan gradient", x, la, B, C, h0, dy), _scan_plan, (x, la, B, C, h0, dy))
+        dx, dla, db, dc = (torch.empty(t.shape, dtype=t.dtype, device=plan.device)
+                           for t in (x, la, B, C))
+        dh0 = torch.empty_like(h0) if h0 is not None and ctx.needs_input_grad[4] else None
         w = _buffer(plan.grad_space, plan.device)
         _check(_lib.fesc_clear_scan_bwd(
             plan.ref, x.data_ptr(), la.data_ptr(), B.data_ptr(), C.data_ptr(), _p(h0),
@@ -358,8 +358,9 @@ def _norm_plan(arrays, vectors, eps, grads=()):
     d = _NormDesc(_TYPES[first.dtype], w, first.numel() // w if w else 0, eps)
     for what, t in arrays:
         setattr(d, what + "_row", _rows(t, what))
+    d.du_row = d.dr_row = w                 # of contiguous gradients, unless given
     for what, t in grads:
-        setattr(d, what + "_row", _rows(t, what) if t is not None else 0)
+        setattr(d, what + "_row", _rows(t, what) if t is not None else w)
     plan = _Plan(d, first.device)
     plan.grad_space = _space(_lib.fesc_clear_norm_workspace, plan.ref)
     plan.shapes = tuple(first.shape)
@@ -382,7 +383,7 @@ def _gated_forward(plan, m, x, z, skip, w):
 class _Gated(torch.autograd.Function):
     @staticmethod
     def forward(ctx, m, x, z, skip, w, eps, plan):
-        ctx.eps = eps
+        ctx.eps, ctx.plan = eps, plan
         ctx.save_for_backward(m, x, z, skip, w)
         return _gated_forward(plan, m, x, z, skip, w)
 
@@ -390,9 +391,12 @@ class _Gated(torch.autograd.Function):
     def backward(ctx, du):
         _once()
         saved = m, x, z, skip, w = ctx.saved_tensors
-        du = _even(du)
-        plan = _plan((ctx.eps, _key("gated gradient", *saved, du)), _gated_plan,
-                     (*saved, ctx.eps, du))
+        if du.is_contiguous():
+            plan = ctx.plan
+        else:
+            du = _even(du)
+            plan = _plan((ctx.eps, _key("gated gradient", *saved, du)), _gated_plan,
+                         (*saved, ctx.eps, du))
         dm, dx, dz, dskip, dw = (torch.empty(t.shape, dtype=t.dtype, device=plan.device)
                                  for t in saved)
         ws = _buffer(plan.grad_space, plan.device)
@@ -436,7 +440,7 @@ class _Residual(torch.autograd.Function):
     @staticmethod
     def forward(ctx, o, r, scale, w, eps, plan):
         ctx.set_materialize_grads(False)
-        ctx.eps = eps
+        ctx.eps, ctx.plan = eps, plan
         ctx.save_for_backward(o, r, scale, w)
         return _residual_forward(plan, o, r, scale, w)
 
@@ -446,10 +450,13 @@ class _Residual(torch.autograd.Function):
         saved = o, r, scale, w = ctx.saved_tensors
         if dnew is None and du is None:
             return (None,) * 6
-        du = _even(du) if du is not None else None
-        dnew = _even(dnew) if dnew is not None else None
-        plan = _plan((ctx.eps, _key("residual gradient", *saved, dnew, du)), _residual_plan,
-                     (*saved, ctx.eps, dnew, du))
+        if (du is None or du.is_contiguous()) and (dnew is None or dnew.is_contiguous()):
+            plan = ctx.plan
+        else:
+            du = _even(du) if du is not None else None
+            dnew = _even(dnew) if dnew is not None else None
+            plan = _plan((ctx.eps, _key("residual gradient", *saved, dnew, du)), _residual_plan,
+                         (*saved, ctx.eps, dnew, du))
         do, dr, dscale, dw = (torch.empty(t.shape, dtype=t.dtype, device=plan.device)
                               for t in saved)
         ws = _buffer(plan.grad_space, plan.device)

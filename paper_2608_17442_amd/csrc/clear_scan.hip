@@ -954,7 +954,7 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   __syncthreads();
 
   // waves 0..3: tiles (s = 16 j + 4 g + i, r = 16 tile + col) of G and W;
-  // waves 4..7: (n = 16 t + 4 g + i, token 16 tile + col) of dC and dB
+  // waves 4..7: (n = state_col(t, g) + i, token 16 tile + col) of dC and dB
   f32x4 gt[4], wk[4];
   f32x4 dc[NT / 16], db[NT / 16];
 #pragma unroll
@@ -972,6 +972,38 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
       }
     }
   }
+  // Waves 4..7: out += scale (state in LDS)^T tok for this wave's 16 tokens, and
+  // into `to` the products of what was added with the tokens' rows of `rowsn`.
+  // Entries lie as in the recurrence's kernels: tiles 2 q and 2 q + 1 together
+  // are those of one row access.
+  auto sum_state = [&](f32x4(&out)[NT / 16], const T* tok, const T* rowsn, float scale,
+                       float* to) {
+    Frag tf[PT / 32];
+#pragma unroll
+    for (int q = 0; q < PT / 32; ++q) tf[q] = row_frag(tok + (16 * tile + col) * XS + 32 * q + 8 * g);
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < NT / 16; t += 2) {
+      f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+      for (int q = 0; q < PT / 32; ++q) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          acc[e] = mma(join(state_four(sr, NS, 32 * q + 8 * g, t + e),
+                            state_four(sr, NS, 32 * q + 8 * g + 4, t + e)), tf[q], acc[e]);
+      }
+      const Frag row = row_frag(rowsn + (16 * tile + col) * NS + 16 * t + 8 * g);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const f32x4 rv = half(row, e);
+        acc[e] *= scale;
+        out[t + e] += acc[e];
+        sum += (acc[e][0] * rv[0] + acc[e][1] * rv[1]) + (acc[e][2] * rv[2] + acc[e][3] * rv[3]);
+      }
+    }
+    sum = sum_groups(sum);
+    if (g == 0) to[16 * tile + col] = sum;
+  };
   // dla of round k, by one wave, from what the waves left in LDS
   float dla = 0.0f;  // token `lane`, summed over the channel tiles of a head
   auto finish = [&](uint32_t k) {
@@ -1030,14 +1062,17 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
     if (left) {
       const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
       float cols = 0.0f;
+      Frag xf[PT / 32];
+#pragma unroll
+      for (int q = 0; q < PT / 32; ++q)
+        xf[q] = row_frag(xs + (16 * tile + col) * XS + 32 * q + 8 * g);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         f32x4 m = {0, 0, 0, 0}, e = {0, 0, 0, 0};
         if (j >= tile) {
 #pragma unroll
-          for (int q = 0; q < PT; q += 32)
-            m = mma(row_frag(dys + (16 * j + col) * XS + q + 8 * g),
-                    row_frag(xs + (16 * tile + col) * XS + q + 8 * g), m);
+          for (int q = 0; q < PT / 32; ++q)
+            m = mma(row_frag(dys + (16 * j + col) * XS + 32 * q + 8 * g), xf[q], m);
           const f32x4 hs = *reinterpret_cast<const f32x4*>(hi + 16 * j + 4 * g);
           const f32x4 ls = *reinterpret_cast<const f32x4*>(lo + 16 * j + 4 * g);
 #pragma unroll
@@ -1060,23 +1095,7 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
       cols = sum_groups(cols);
       if (g == 0) colsum[now][16 * tile + col] = cols;
     } else {
-      const float es = ec[16 * tile + col];
-      float sum = 0.0f;
-#pragma unroll
-      for (int t = 0; t < NT / 16; ++t) {
-        f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-        for (int q = 0; q < PT; q += 32)
-          acc = mma(join(col_four(sr, NS, q + 8 * g, 16 * t), col_four(sr, NS, q + 8 * g + 4, 16 * t)),
-                    row_frag(dys + (16 * tile + col) * XS + q + 8 * g), acc);
-        acc *= es;
-        dc[t] += acc;
-        const f32x4 cv =
-            widen(*reinterpret_cast<const Four*>(cs + (16 * tile + col) * NS + 16 * t + 4 * g));
-        sum += (acc[0] * cv[0] + acc[1] * cv[1]) + (acc[2] * cv[2] + acc[3] * cv[3]);
-      }
-      sum = sum_groups(sum);
-      if (g == 0) us[now][16 * tile + col] = sum;
+      sum_state(dc, dys, cs, ec[16 * tile + col], us[now]);
     }
     if (k + 1 < rounds) fetch_state(k + 1);
     __syncthreads();
@@ -1092,42 +1111,35 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
       const Mem dx((T*)a.dx + (((uint64_t)b * sh.len + t0) * sh.heads + h) * P + p0);
       const uint32_t at = (16 * tile + col) * sh.heads * P * (uint32_t)sizeof(T);
 #pragma unroll
-      for (int x = 0; x < PT / 16; ++x) {
-        f32x4 acc = {0, 0, 0, 0};
+      for (int x = 0; x < PT / 16; x += 2) {
+        f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-        for (int q = 0; q < NT / 32; ++q)
-          acc = mma(row_frag(sr + (16 * x + col) * NS + 32 * q + 8 * g), bf[q], acc);
-        acc *= wr;
+        for (int q = 0; q < NT / 32; ++q) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            acc[e] = mma(row_frag(sr + (16 * (x + e) + col) * NS + 32 * q + 8 * g), bf[q], acc[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) acc[e] *= wr;
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
           if (j + 1 >= tile) {
-            const Frag df = join(col_four(dys, XS, 16 * j + 4 * g, 16 * x),
-                                 col_four(dys, XS, 16 * j + 16 + 4 * g, 16 * x));
-            acc = mma(df, join(dg[j], dg[j + 1]), acc);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              acc[e] = mma(join(col_four(dys, XS, 16 * j + 4 * g, 16 * (x + e)),
+                                col_four(dys, XS, 16 * j + 16 + 4 * g, 16 * (x + e))),
+                           join(dg[j], dg[j + 1]), acc[e]);
           }
         }
-        const int pp = 16 * x + 4 * g;
-        dx.store_four<T, VEC>(at + pp * (uint32_t)sizeof(T), acc,
-                              16 * tile + col < n ? rows - pp : 0);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int pp = 16 * (x + e) + 4 * g;
+          dx.store_four<T, VEC>(at + pp * (uint32_t)sizeof(T), acc[e],
+                                16 * tile + col < n ? rows - pp : 0);
+        }
       }
     } else {
-      const float wr = wt[16 * tile + col];
-      float sum = 0.0f;
-#pragma unroll
-      for (int t = 0; t < NT / 16; ++t) {
-        f32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-        for (int q = 0; q < PT; q += 32)
-          acc = mma(join(col_four(sr, NS, q + 8 * g, 16 * t), col_four(sr, NS, q + 8 * g + 4, 16 * t)),
-                    row_frag(xs + (16 * tile + col) * XS + q + 8 * g), acc);
-        acc *= wr;
-        db[t] += acc;
-        const f32x4 bv =
-            widen(*reinterpret_cast<const Four*>(bs + (16 * tile + col) * NS + 16 * t + 4 * g));
-        sum += (acc[0] * bv[0] + acc[1] * bv[1]) + (acc[2] * bv[2] + acc[3] * bv[3]);
-      }
-      sum = sum_groups(sum);
-      if (g == 0) vs[now][16 * tile + col] = sum;
+      sum_state(db, xs, bs, wt[16 * tile + col], vs[now]);
     }
     if (wave == kSums && k + 1 < rounds) cum = cumulate(lav);
   }
@@ -1157,12 +1169,12 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   for (int x = 0; x < NT / 16; ++x) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      dc[x] = mma(join(col_four(bs, NS, 32 * q + 8 * g, 16 * x),
-                       col_four(bs, NS, 32 * q + 8 * g + 4, 16 * x)), wc[q], dc[x]);
-      db[x] = mma(join(col_four(cs, NS, 32 * q + 8 * g, 16 * x),
-                       col_four(cs, NS, 32 * q + 8 * g + 4, 16 * x)), wb[q], db[x]);
+      dc[x] = mma(join(state_four(bs, NS, 32 * q + 8 * g, x),
+                       state_four(bs, NS, 32 * q + 8 * g + 4, x)), wc[q], dc[x]);
+      db[x] = mma(join(state_four(cs, NS, 32 * q + 8 * g, x),
+                       state_four(cs, NS, 32 * q + 8 * g + 4, x)), wb[q], db[x]);
     }
-    const int nn = 16 * x + 4 * g;
+    const int nn = state_col(x, g);
     const uint32_t at = (16 * tile + col) * sh.groups * N + nn;
     const int some = 16 * tile + col < n ? N - nn : 0;
     if (a.db_part) {

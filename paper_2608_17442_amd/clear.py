@@ -306,6 +306,8 @@ def scan_step(x, la, B, C, state, slots=None, stream=None):
     _check(_lib.fesc_clear_scan_step(plan.ref, x.data_ptr(), la.data_ptr(), B.data_ptr(),
                                      C.data_ptr(), state.data_ptr(), state.shape[0], _p(slots),
                                      y.data_ptr(), _stream(device.index)))
+    # a gradient that was to read the states as they were is refused
+    torch.autograd.graph.increment_version(state)
     return y
 
 

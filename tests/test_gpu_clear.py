@@ -291,6 +291,18 @@ def test_steps_go_on_from_a_scan(clear, dtype):
     check(h, hw, dtype, "h")
 
 
+def test_step_is_seen_by_autograd(clear):
+    """A gradient that needs the state from before a step in place is refused."""
+    step("step between a scan and its gradient")
+    x, la, B, C = dev(*R.factors(25, 2, 5, 3, 16, 1, 32, F32))
+    state = torch.zeros(2, 3, 16, 32, device="cuda")
+    y = clear.scan(x.requires_grad_(), la, B, C, state)
+    with torch.no_grad():
+        clear.scan_step(x[:, 0], la[:, 0], B[:, 0], C[:, 0], state)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
 def test_step_past_32_bit_offsets(clear):
     """A pool of more than 2^32 state entries."""
     step("step in a large pool")

@@ -61,19 +61,47 @@ struct Rows {
 };
 
 // How a pass over the sequence is cut.  A workgroup carries the states of its
-// channel tiles from chunk to chunk.  With many tiles each takes its sequence as
-// a whole, in workgroups of eight waves.  With fewer the sequence is cut into
-// segments of whole chunks (a segment's pass over its own tokens is the price: x
-// and B are read twice): in workgroups of two tiles, which share what is read of
-// B and C, where segments of four chunks still fill the chip; of one tile and
-// shorter segments, two chunks at least, where they do not.
-// `dirs`: passes that run at once.
-constexpr uint64_t kWholeTiles = 160;   // tiles that occupy most of 256 compute units
-constexpr uint64_t kPairGroups = 512;   // workgroups of pairs, two on each unit
-constexpr uint64_t kShortGroups = 256;  // workgroups of one tile
+// channel tiles from chunk to chunk; of the tiles there are
+// batch * heads * (directions that run at once), and 256 compute units take one
+// or, at some 1.75 times the time of a chunk, two workgroups each (one in
+// float32, whose LDS tiles are twice the size).
+//  - Many tiles: each takes its sequence as a whole, eight waves, one launch.
+//  - Otherwise segments of whole chunks; the price is a pass before, in which x and
+//    B are read for the segments' own states, and their join.  Two workgroups a
+//    unit where segments of six chunks remain, else one, two chunks at least.
+//  - Long sequences: segments in workgroups of two tiles (four waves), which
+//    share what is read of B and C and the product of the two.
+// Measured with 24 heads of 64, state 128, bfloat16, in us, forward:
+//    tiles x chunks   whole   one a unit   two a unit   pairs
+//     24 x 32           79       33            -          59
+//     48 x 32           79       43           49          55
+//     96 x 32           81       72           59          69
+//    144 x 32           81        -           77          82
+//    168 x 32           83        -           79          92
+//    192 x 32           82        -          104          96
+//     24 x 128         303       67           63          73
+//     48 x 128         303      112           98         100
+//     96 x 128         303      250          168         157
+//    144 x 128         306        -          262         216
+//    192 x 128         333        -          365         299
+//     24 x 782           -      275            -         242
+// The gradient's pass carries states in both directions, so that a cut doubles its
+// work (whole gradient call, tiles of both directions):
+//     48 x 32           77       59           62          68
+//     96 x 32           89       94           84          92
+//    144 x 32          112        -          118         128
+//    192 x 32          115        -          139         135
+//     48 x 128         244      147          134         142
+//     48 x 256         516      304          266         257
+constexpr uint64_t kUnits = 256;
+constexpr uint64_t kWholeTiles = 171, kWholeTilesGrad = 96;  // whole from here on
+constexpr uint64_t kTwoChunks = 2 * kUnits * 6;      // tiles * chunks for two a unit
+constexpr uint64_t kPairChunks = 8192;               // tiles * chunks for pairs
+constexpr uint64_t kPairTiles = 256;
 // Up to this many segments each workgroup adds up the summaries before its own
 // (segs / 2 states read on average); more go through the join kernel (each read
-// and written once, a launch more).
+// and written once, a launch more).  24 tiles x 32 chunks in 3 segments: 50.3 us
+// against 52.5 with the kernel; 5: 38.8, 40.5; 6: 36.7, 37.3; 8: 36.4, 34.0.
 constexpr uint32_t kJoinedSegs = 5;
 ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   ScanShape s{};
@@ -91,13 +119,16 @@ ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   const bool pairs = d->dtype == FESC_BF16 && d->heads / d->groups * s.ptiles % 2 == 0;
   uint64_t segs = 1;
   s.tiles = 1;
-  if (tiles && tiles < kWholeTiles) {
-    if (pairs && tiles / 2 * (s.chunks / 4) >= kPairGroups) {
-      s.tiles = 2;
-      segs = kPairGroups / (tiles / 2);
-    } else {
-      segs = std::min<uint64_t>(kShortGroups / tiles, std::max<uint32_t>(1, s.chunks / 2));
-    }
+  const uint64_t whole = dirs == 1 ? kWholeTiles : kWholeTilesGrad;
+  const uint64_t work = tiles * s.chunks;
+  if (tiles && pairs && tiles < (dirs == 1 ? kPairTiles : whole) && work >= kPairChunks) {
+    s.tiles = 2;
+    segs = 2 * kUnits / (tiles / 2);
+  } else if (tiles && tiles < whole) {
+    if (d->dtype == FESC_BF16 && work >= kTwoChunks)
+      segs = 2 * kUnits / tiles;
+    else
+      segs = std::max<uint64_t>(1, std::min<uint64_t>(kUnits / tiles, s.chunks / 2));
   }
   s.seg_chunks = (uint32_t)((s.chunks + segs - 1) / segs);
   s.segs = s.chunks ? (s.chunks + s.seg_chunks - 1) / s.seg_chunks : 1;
@@ -105,12 +136,15 @@ ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   return s;
 }
 
-// Heads of a group in turn in one workgroup of the gradient kernel; split
-// over workgroups where chunks alone are too few.
+// Heads of a group in turn in one workgroup of the gradient kernel (one on a
+// unit); split over workgroups, whose parts of dB and dC are added up, where
+// chunks alone leave units idle.  Whole gradient call, 24 heads, in us: 32 chunks in
+// 4, 8, 12 splits 68, 60, 69; 64 in 2, 4, 8: 115, 95, 104; 128 in 1, 2, 4: 154, 116,
+// 126; 192 in 1, 2: 193, 216.
 void split_heads(const ScanShape& s, uint32_t* splits, uint32_t* per) {
   const uint32_t heads = s.heads / s.groups;
   const uint64_t groups = (uint64_t)s.batch * s.chunks * s.groups;
-  const uint64_t want = std::min<uint64_t>(heads, groups ? (256 + groups - 1) / groups : 1);
+  const uint64_t want = std::min<uint64_t>(heads, std::max<uint64_t>(1, groups ? kUnits / groups : 1));
   *per = (uint32_t)((heads + want - 1) / want);
   *splits = (heads + *per - 1) / *per;
 }

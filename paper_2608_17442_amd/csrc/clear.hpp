@@ -98,7 +98,6 @@ hipError_t launch_state_copy(const float* from, float* to, uint64_t count, hipSt
 hipError_t launch_norm(uint32_t dtype, bool gated, const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_grad(uint32_t dtype, bool gated, const NormArgs& a, hipStream_t s);
 // Workgroups of the gradient kernel, each with a row of partial sums.
-constexpr uint32_t kNormGradBlocks = 1024;
 uint32_t norm_grad_blocks(uint64_t rows, uint32_t width, bool vec);
 
 }  // namespace fesc

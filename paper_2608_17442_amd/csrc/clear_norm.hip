@@ -400,7 +400,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_parts(NormArgs a) {
 }
 
 // Lanes that share a row, by its units (unaligned rows: at least 256 lanes,
-// whose loads go element by element anyway).
+// whose loads go element by element anyway).  The gradient at 1536 channels, 16384
+// rows: 128 lanes of two units, with the next row's loads under way, 59 us; 256 of
+// one 122; 64 of three, without, 149.
 uint32_t lanes_of(uint32_t width, bool vec) {
   const uint32_t units = (width + kUnit - 1) / kUnit;
   return units <= 64 || (units <= 128 && vec) ? 64 : units <= 256 && vec ? 128 : 256;
@@ -435,16 +437,22 @@ hipError_t norm(const NormArgs& a, uint32_t blocks, hipStream_t s) {
 
 }  // namespace
 
+// Workgroups of a gradient: two on a compute unit, each of which leaves a row of
+// partial sums; one for wide rows, whose partial sums weigh most.  16384 rows of
+// 1536, 256, 512, 1024 workgroups: 66, 60, 64 us; 4096 rows of 1536: 22.7, 21.8, 26;
+// 4096 of 4096: 43, 47, 61; 4096 of 8192: 103, 116, 145.
 uint32_t norm_grad_blocks(uint64_t rows, uint32_t width, bool vec) {
   const uint32_t at_once = kThreads / lanes_of(width, vec);
-  const uint64_t n = (rows + at_once - 1) / at_once;
-  return (uint32_t)(n < kNormGradBlocks ? n : kNormGradBlocks);
+  const uint64_t n = (rows + at_once - 1) / at_once, most = width < 4096 ? 512 : 256;
+  return (uint32_t)(n < most ? n : most);
 }
 
 hipError_t launch_norm(uint32_t dtype, bool gated, const NormArgs& a, hipStream_t s) {
   const uint32_t at_once = kThreads / lanes_of(a.width, a.vec);
   const uint64_t n = (a.rows + at_once - 1) / at_once;
-  const uint32_t blocks = (uint32_t)(n < 4096 ? n : 4096);
+  // 16384 rows of 1536: 4096 workgroups 31.8 us, 8192 30.6; 65536 of 384: 32.3, 31.5,
+  // 16384 30.6
+  const uint32_t blocks = (uint32_t)(n < 16384 ? n : 16384);
   if (dtype == FESC_BF16)
     return gated ? norm<__bf16, true, false>(a, blocks, s) : norm<__bf16, false, false>(a, blocks, s);
   return gated ? norm<float, true, false>(a, blocks, s) : norm<float, false, false>(a, blocks, s);

@@ -104,6 +104,40 @@ def test_scan_gradient(clear, shape, dtype, state):
         check(a, w, dtype, n)
 
 
+# the ways to cut a bfloat16 sequence: whole; segments, one and two workgroups
+# on a compute unit; segments of two channel tiles
+CUTS = [(8, 130, 24, 16, 2, 16), (3, 700, 20, 16, 1, 16), (5, 1960, 20, 16, 1, 16),
+        (4, 5490, 24, 16, 2, 16), (2, 5500, 24, 128, 1, 16)]
+
+
+@pytest.mark.parametrize("shape", CUTS)
+@pytest.mark.parametrize("state", [False, True])
+def test_scan_cuts(clear, shape, state):
+    step(f"scan cuts {shape} state={state}")
+    b, L, H, P, G, N = shape
+    f = dev(*R.factors(7, *shape, BF16, resets=[L // 2]))
+    h0 = torch.randn(b, H, P, N, device="cuda") if state else None
+    got = clear.scan(*f, h0=h0, return_state=state)
+    want, hw = (t.cpu() for t in R.scan(*wide(*f, h0)))
+    y, h = got if state else (got, None)
+    check(y, want, BF16, "y")
+    if state:
+        check(h, hw, BF16, "h")
+
+
+@pytest.mark.parametrize("shape", [(3, 300, 20, 16, 2, 8), (1, 1300, 20, 16, 1, 8),
+                                   (1, 4490, 22, 16, 1, 8), (1, 12000, 22, 16, 1, 8)])
+def test_scan_gradient_cuts(clear, shape):
+    step(f"scan gradient cuts {shape}")
+    f = [t.requires_grad_() for t in dev(*R.factors(8, *shape, BF16))]
+    dy = torch.randn(shape[:4], device="cuda").to(BF16)
+    got = torch.autograd.grad(clear.scan(*f), f, dy)
+    leaves = [t.detach().double().requires_grad_() for t in f]
+    want = torch.autograd.grad(R.scan(*leaves)[0], leaves, dy.double())
+    for n, a, w in zip(("dx", "dla", "dB", "dC"), got, want):
+        check(a, w.cpu(), BF16, n)
+
+
 def test_scan_gradient_against_differences(clear):
     """<gradient, direction> against the central difference of the definition
     in 64 bits, whose error is some 1e-9 here."""

@@ -888,13 +888,18 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   constexpr int XS = PT + Elem<T>::kPad, NS = NT + Elem<T>::kPad;
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
-  __shared__ __align__(16) T xs[Q * XS];
-  __shared__ __align__(16) T dys[Q * XS];
-  __shared__ __align__(16) T sr[PT * NS];
-  __shared__ __align__(16) float hi[Q], lo[Q], ec[Q], wt[Q];
-  // of the head at hand and of the one before, whose dla is still to be formed
-  __shared__ float us[2][Q], vs[2][Q], colsum[2][Q], rowsum[2][4][Q], dots[2][8], total[2];
-  __shared__ bool reset[2][Q];
+  // Rounds lie in turn in two places, S and R side by side: one barrier each.  In
+  // float32 LDS has room for one place, R following S in it.
+  constexpr bool kTwice = sizeof(T) == 2;
+  constexpr int kPlaces = kTwice ? 2 : 1;
+  __shared__ __align__(16) T x_s[kPlaces][Q * XS];
+  __shared__ __align__(16) T dy_s[kPlaces][Q * XS];
+  __shared__ __align__(16) T s_s[kPlaces * kPlaces][PT * NS];
+  __shared__ __align__(16) float hi_s[2][Q], lo_s[2][Q], ec_s[2][Q], wt_s[2][Q];
+  // of the round at hand and of the one before, whose dla is still to be formed;
+  // what is written before a round's barrier, also of the round to come
+  __shared__ float us[2][Q], vs[2][Q], colsum[2][Q], rowsum[2][4][Q], dots[4][8], total[4];
+  __shared__ bool reset[4][Q];
   using Frag = typename Elem<T>::Frag;
   using Four = typename Elem<T>::Four;
   const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
@@ -978,8 +983,8 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   // into `to` the products of what was added with the tokens' rows of `rowsn`.
   // Entries lie as in the recurrence's kernels: tiles 2 q and 2 q + 1 together
   // are those of one row access.
-  auto sum_state = [&](f32x4(&out)[NT / 16], const T* tok, const T* rowsn, float scale,
-                       float* to) {
+  auto sum_state = [&](f32x4(&out)[NT / 16], const T* sr, const T* tok, const T* rowsn,
+                       float scale, float* to) {
     Frag tf[PT / 32];
 #pragma unroll
     for (int q = 0; q < PT / 32; ++q) tf[q] = row_frag(tok + (16 * tile + col) * XS + 32 * q + 8 * g);
@@ -1009,10 +1014,10 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   // dla of round k, by one wave, from what the waves left in LDS
   float dla = 0.0f;  // token `lane`, summed over the channel tiles of a head
   auto finish = [&](uint32_t k) {
-    const int b2 = k & 1;
+    const int b2 = k & 1, b4 = k & 3;
     float base = 0.0f;
 #pragma unroll
-    for (int x = 0; x < 8; ++x) base += dots[b2][x];
+    for (int x = 0; x < 8; ++x) base += dots[b4][x];
     const float u = us[b2][lane] +
                     ((rowsum[b2][0][lane] + rowsum[b2][1][lane]) +
                      (rowsum[b2][2][lane] + rowsum[b2][3][lane])) -
@@ -1027,7 +1032,7 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
     }
     const float upto = __shfl_up(before, 1);
     // before a reset nothing counts: the exact zero, not the sums' remainder
-    dla += reset[b2][lane] ? 0.0f : after + (lane ? upto : 0.0f) + base * total[b2];
+    dla += reset[b4][lane] ? 0.0f : after + (lane ? upto : 0.0f) + base * total[b4];
     if (k % sh.ptiles + 1 == sh.ptiles) {
       const uint32_t h = grp * per_group + h0 + k / sh.ptiles;
       if (lane < n) ((T*)a.dla)[((uint64_t)b * sh.len + t0 + lane) * sh.heads + h] = (T)dla;
@@ -1043,20 +1048,25 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   for (uint32_t k = 0; k < rounds; ++k) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
     const int p0 = pt * PT, rows = min(PT, P - p0), now = k & 1;
-    __syncthreads();
+    const int place = kTwice ? now : 0, at4 = k & 3;
+    T *xs = x_s[place], *dys = dy_s[place], *sr = s_s[kPlaces * place];
+    T* rr = s_s[kPlaces * place + kPlaces - 1];
+    float *hi = hi_s[now], *lo = lo_s[now], *ec = ec_s[now], *wt = wt_s[now];
+    if constexpr (!kTwice) __syncthreads();
     xst.store(xs, XS);
     dyst.store(dys, XS);
     sst.store(sr, NS);
+    if constexpr (kTwice) rst.store(rr, NS);
     if (wave == kSums) {
       hi[lane] = cum.hi;
       lo[lane] = cum.lo;
       ec[lane] = cum.e;
       wt[lane] = cum.w;
-      reset[now][lane] = lav < kReset;
-      if (lane == 0) total[now] = cum.total;
+      reset[at4][lane] = lav < kReset;
+      if (lane == 0) total[at4] = cum.total;
     }
     const float dot = sum_groups(sum16(rst.dot(sst)));
-    if (lane == 0) dots[now][wave] = dot;
+    if (lane == 0) dots[at4][wave] = dot;
     __syncthreads();
     if (k + 1 < rounds) fetch_tokens(k + 1);
     if (wave == kFinish && k) finish(k - 1);
@@ -1097,12 +1107,14 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
       cols = sum_groups(cols);
       if (g == 0) colsum[now][16 * tile + col] = cols;
     } else {
-      sum_state(dc, dys, cs, ec[16 * tile + col], us[now]);
+      sum_state(dc, sr, dys, cs, ec[16 * tile + col], us[now]);
     }
     if (k + 1 < rounds) fetch_state(k + 1);
-    __syncthreads();
-    rst.store(sr, NS);
-    __syncthreads();
+    if constexpr (!kTwice) {
+      __syncthreads();
+      rst.store(rr, NS);
+      __syncthreads();
+    }
     if (k + 1 < rounds) fetch_adjoint(k + 1);
     if (left) {
       const float wr = wt[16 * tile + col];
@@ -1119,7 +1131,7 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
         for (int q = 0; q < NT / 32; ++q) {
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            acc[e] = mma(row_frag(sr + (16 * (x + e) + col) * NS + 32 * q + 8 * g), bf[q], acc[e]);
+            acc[e] = mma(row_frag(rr + (16 * (x + e) + col) * NS + 32 * q + 8 * g), bf[q], acc[e]);
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) acc[e] *= wr;
@@ -1141,12 +1153,13 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
         }
       }
     } else {
-      sum_state(db, xs, bs, wt[16 * tile + col], vs[now]);
+      sum_state(db, rr, xs, bs, wt[16 * tile + col], vs[now]);
     }
     if (wave == kSums && k + 1 < rounds) cum = cumulate(lav);
   }
   __syncthreads();
   if (wave == kFinish) finish(rounds - 1);
+  T* xs = x_s[0];
   // W to LDS (rows s, columns r), then its products with B and C
   if (left) {
 #pragma unroll

@@ -16,6 +16,7 @@
 // inputs enter as bf16 parts, three that sum to the fp32 value exactly where the
 // state (or its gradient) is an output of the call, otherwise two.
 #include <algorithm>
+#include <type_traits>
 
 #include "clear.hpp"
 #include "clear_mem.hpp"
@@ -158,14 +159,15 @@ __device__ __forceinline__ float load1(const T* p) {
 
 // Where a thread's units of a ROWS x COLS tile lie in memory.  VEC: rows start
 // at multiples of 16 bytes and do not overlap, so that one offset, formed once,
-// and the bytes that the valid rows span say all.
-template <typename T, int COLS, int THREADS, bool VEC>
+// and the bytes that the valid rows span say all.  FIRST: the first thread of those
+// that share the work.
+template <typename T, int COLS, int THREADS, bool VEC, int FIRST = 0>
 struct Rows {
   uint32_t pitch, first, step;
   int cols;
   __device__ __forceinline__ Rows(uint32_t pitch_, int cols_) : pitch(pitch_), cols(cols_) {
     constexpr int kUnit = Elem<T>::kUnit, kPerRow = COLS / kUnit;
-    const int row = threadIdx.x / kPerRow, col = threadIdx.x % kPerRow * kUnit;
+    const int row = (threadIdx.x - FIRST) / kPerRow, col = (threadIdx.x - FIRST) % kPerRow * kUnit;
     first = col < cols ? (row * pitch + col) * (uint32_t)sizeof(T) : kAbsent;
     step = THREADS / kPerRow * pitch * (uint32_t)sizeof(T);
   }
@@ -176,13 +178,13 @@ struct Rows {
 
 // Registers of one thread for a tile of ROWS x COLS elements on its way from
 // global memory to LDS; rows and columns past the valid ones are zero.
-template <typename T, int ROWS, int COLS, int THREADS, bool VEC>
+template <typename T, int ROWS, int COLS, int THREADS, bool VEC, int FIRST = 0>
 struct Stage {
   static constexpr int kUnit = Elem<T>::kUnit;
   static constexpr int kPerRow = COLS / kUnit;
   static constexpr int kUnits = ROWS * kPerRow / THREADS;
   static_assert(ROWS * kPerRow % THREADS == 0, "whole units per thread");
-  using In = Rows<T, COLS, THREADS, VEC>;
+  using In = Rows<T, COLS, THREADS, VEC, FIRST>;
   u32x4 r[kUnits];
 
   __device__ __forceinline__ void load(const T* base, const In& in, int rows) {
@@ -194,7 +196,7 @@ struct Stage {
       const Mem m(base);
 #pragma unroll
       for (int k = 0; k < kUnits; ++k) {
-        const int i = threadIdx.x + k * THREADS;
+        const int i = (threadIdx.x - FIRST) + k * THREADS;
         const int row = i / kPerRow, col = i % kPerRow * kUnit;
         const uint32_t at = (row * in.pitch + col) * (uint32_t)sizeof(T);
         u32x4 v = {0, 0, 0, 0};
@@ -214,14 +216,14 @@ struct Stage {
   __device__ __forceinline__ void store(T* tile, int pitch) const {
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-      const int i = threadIdx.x + k * THREADS;
+      const int i = (threadIdx.x - FIRST) + k * THREADS;
       *reinterpret_cast<u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit) = r[k];
     }
   }
   __device__ __forceinline__ void take(const T* tile, int pitch) {
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-      const int i = threadIdx.x + k * THREADS;
+      const int i = (threadIdx.x - FIRST) + k * THREADS;
       r[k] = *reinterpret_cast<const u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit);
     }
   }
@@ -234,7 +236,7 @@ struct Stage {
       const Mem m(base);
 #pragma unroll
       for (int k = 0; k < kUnits; ++k) {
-        const int i = threadIdx.x + k * THREADS;
+        const int i = (threadIdx.x - FIRST) + k * THREADS;
         const int row = i / kPerRow, col = i % kPerRow * kUnit;
         const uint32_t at = (row * out.pitch + col) * (uint32_t)sizeof(T);
 #pragma unroll
@@ -871,6 +873,8 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
 
 // ------------------------------------------------------------ gradient
 
+constexpr int kGradThreads = 768;
+
 // Gradients of one chunk, all heads of a split in turn (their sum is dB and
 // dC).  S the state that enters the chunk, R the adjoint of the one that
 // leaves it, K_{s,r} = dy_s . x_r, G_{s,r} = C_s . B_r, D_{s,r} = e^{cum_s - cum_r}
@@ -881,10 +885,11 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
 //   dla_t = sum_{s >= t > r} (D K G)_{s,r} + sum_{s >= t} C_s . (e^{cum_s} S^T dy_s)
 //           + sum_{r < t} B_r . (w_r R^T x_r) + e^{cum_Q} <R, S>
 // The first sum of dla falls from t to t + 1 by row sum minus column sum of
-// D K G at t.  Waves 0..3 hold the 16 columns r of G, K and W and form dx;
-// waves 4..7 hold 16 tokens of dC and dB.
+// D K G at t.  Wave w of 0..3 holds the columns r = 16 w ... of G, K and W
+// and forms dx; wave 4 + 4 e + w holds half e of the entries of dC and dB for the
+// tokens 16 w ....
 template <typename T, int NT, bool VEC>
-__global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
+__global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGrad a) {
   constexpr int XS = PT + Elem<T>::kPad, NS = NT + Elem<T>::kPad;
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
@@ -898,7 +903,7 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   __shared__ __align__(16) float hi_s[2][Q], lo_s[2][Q], ec_s[2][Q], wt_s[2][Q];
   // of the round at hand and of the one before, whose dla is still to be formed;
   // what is written before a round's barrier, also of the round to come
-  __shared__ float us[2][Q], vs[2][Q], colsum[2][Q], rowsum[2][4][Q], dots[4][8], total[4];
+  __shared__ float us[2][2][Q], vs[2][2][Q], colsum[2][Q], rowsum[2][4][Q], dots[4][8], total[4];
   __shared__ bool reset[4][Q];
   using Frag = typename Elem<T>::Frag;
   using Four = typename Elem<T>::Four;
@@ -916,58 +921,75 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   const uint32_t hn = min(a.heads_per_split, per_group - h0);
   const uint64_t size = (uint64_t)P * N;
 
-  {
-    using NStage = Stage<T, Q, NT, 512, VEC>;
-    NStage st;
+  // Waves 0..3 bring x and dy of a round, the others S and R.
+  using XStage = Stage<T, Q, PT, 256, VEC>;
+  using SStage = Stage<T, PT, NT, 512, VEC, 256>;
+  constexpr int kUnits = XStage::kUnits > SStage::kUnits ? XStage::kUnits : SStage::kUnits;
+  u32x4 one[kUnits], two[kUnits];
+  if (!left) {
+    using NStage = Stage<T, Q, NT, 512, VEC, 256>;
+    NStage st, st2;
     st.load((const T*)a.b + b * a.b_batch + t0 * a.b_token + (int64_t)grp * N,
             typename NStage::In(a.b_token, N), n);
+    st2.load((const T*)a.c + b * a.c_batch + t0 * a.c_token + (int64_t)grp * N,
+             typename NStage::In(a.c_token, N), n);
     st.store(bs, NS);
-    st.load((const T*)a.c + b * a.c_batch + t0 * a.c_token + (int64_t)grp * N,
-            typename NStage::In(a.c_token, N), n);
-    st.store(cs, NS);
+    st2.store(cs, NS);
   }
-  using XStage = Stage<T, Q, PT, 512, VEC>;
-  using SStage = Stage<T, PT, NT, 512, VEC>;
-  XStage xst, dyst;
-  SStage sst, rst;
   float lav = 0.0f;
   const uint32_t la_at =
       lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent;
-  // the loads of round k (head of the split and channel tile), in portions that
-  // do not hold the work up
-  auto fetch_tokens = [&](uint32_t k) {
+  // the loads of round k (head of the split and channel tile): la, x and S, then
+  // dy and R
+  auto tokens = [&](const void* base, uint64_t batch, uint64_t token, uint32_t k, u32x4* r) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
-    const int p0 = pt * PT, rows = min(PT, P - p0);
-    lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h).load<T>(la_at);
-    xst.load((const T*)a.x + b * a.x_batch + t0 * a.x_token + (int64_t)h * P + p0,
-             typename XStage::In(a.x_token, rows), n);
-    dyst.load((const T*)a.dy + b * a.dy_batch + t0 * a.dy_token + (int64_t)h * P + p0,
-              typename XStage::In(a.dy_token, rows), n);
+    XStage st;
+    st.load((const T*)base + b * batch + t0 * token + (int64_t)h * P + pt * PT,
+            typename XStage::In(token, min(PT, P - (int)pt * PT)), n);
+#pragma unroll
+    for (int u = 0; u < XStage::kUnits; ++u) r[u] = st.r[u];
   };
-  auto state_at = [&](uint32_t k) {
+  auto states = [&](const void* base, uint32_t k, u32x4* r) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
-    return (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size + (uint64_t)pt * PT * N;
+    SStage st;
+    st.load((const T*)base + (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size +
+                (uint64_t)pt * PT * N,
+            typename SStage::In(N, N), min(PT, P - (int)pt * PT));
+#pragma unroll
+    for (int u = 0; u < SStage::kUnits; ++u) r[u] = st.r[u];
   };
-  auto state_rows = [&](uint32_t k) { return min(PT, P - (int)(k % sh.ptiles) * PT); };
-  auto fetch_state = [&](uint32_t k) {
-    sst.load((const T*)a.s_in + state_at(k), typename SStage::In(N, N), state_rows(k));
+  auto fetch_one = [&](auto is_left, uint32_t k) {
+    if constexpr (is_left) {
+      const uint32_t h = grp * per_group + h0 + k / sh.ptiles;
+      lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h).load<T>(la_at);
+      tokens(a.x, a.x_batch, a.x_token, k, one);
+    } else {
+      states(a.s_in, k, one);
+    }
   };
-  auto fetch_adjoint = [&](uint32_t k) {
-    rst.load((const T*)a.r_in + state_at(k), typename SStage::In(N, N), state_rows(k));
+  auto fetch_two = [&](auto is_left, uint32_t k) {
+    if constexpr (is_left)
+      tokens(a.dy, a.dy_batch, a.dy_token, k, two);
+    else
+      states(a.r_in, k, two);
   };
-  fetch_tokens(0);
-  fetch_state(0);
-  fetch_adjoint(0);
+  auto staged = [](auto st, const u32x4* r) {
+#pragma unroll
+    for (int u = 0; u < decltype(st)::kUnits; ++u) st.r[u] = r[u];
+    return st;
+  };
   __syncthreads();
 
   // waves 0..3: tiles (s = 16 j + 4 g + i, r = 16 tile + col) of G and W;
-  // waves 4..7: (n = state_col(t, g) + i, token 16 tile + col) of dC and dB
+  // the others: (n = state_col(first + t, g) + i, token 16 tile + col) of dC and dB
+  constexpr int kOwn = NT / 32;
+  const int half_of = left ? 0 : (wave >> 2) - 1, first = half_of * kOwn;
   f32x4 gt[4], wk[4];
-  f32x4 dc[NT / 16], db[NT / 16];
+  f32x4 dc[kOwn], db[kOwn];
 #pragma unroll
   for (int j = 0; j < 4; ++j) gt[j] = wk[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int t = 0; t < NT / 16; ++t) dc[t] = db[t] = f32x4{0, 0, 0, 0};
+  for (int t = 0; t < kOwn; ++t) dc[t] = db[t] = f32x4{0, 0, 0, 0};
   if (left) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -979,27 +1001,27 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
       }
     }
   }
-  // Waves 4..7: out += scale (state in LDS)^T tok for this wave's 16 tokens, and
+  // out += scale (state in LDS)^T tok for this wave's tokens and entries, and
   // into `to` the products of what was added with the tokens' rows of `rowsn`.
   // Entries lie as in the recurrence's kernels: tiles 2 q and 2 q + 1 together
   // are those of one row access.
-  auto sum_state = [&](f32x4(&out)[NT / 16], const T* sr, const T* tok, const T* rowsn,
+  auto sum_state = [&](f32x4(&out)[kOwn], const T* sr, const T* tok, const T* rowsn,
                        float scale, float* to) {
     Frag tf[PT / 32];
 #pragma unroll
     for (int q = 0; q < PT / 32; ++q) tf[q] = row_frag(tok + (16 * tile + col) * XS + 32 * q + 8 * g);
     float sum = 0.0f;
 #pragma unroll
-    for (int t = 0; t < NT / 16; t += 2) {
+    for (int t = 0; t < kOwn; t += 2) {
       f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
       for (int q = 0; q < PT / 32; ++q) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          acc[e] = mma(join(state_four(sr, NS, 32 * q + 8 * g, t + e),
-                            state_four(sr, NS, 32 * q + 8 * g + 4, t + e)), tf[q], acc[e]);
+          acc[e] = mma(join(state_four(sr, NS, 32 * q + 8 * g, first + t + e),
+                            state_four(sr, NS, 32 * q + 8 * g + 4, first + t + e)), tf[q], acc[e]);
       }
-      const Frag row = row_frag(rowsn + (16 * tile + col) * NS + 16 * t + 8 * g);
+      const Frag row = row_frag(rowsn + (16 * tile + col) * NS + 16 * (first + t) + 8 * g);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const f32x4 rv = half(row, e);
@@ -1018,11 +1040,11 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
     float base = 0.0f;
 #pragma unroll
     for (int x = 0; x < 8; ++x) base += dots[b4][x];
-    const float u = us[b2][lane] +
+    const float u = us[b2][0][lane] + us[b2][1][lane] +
                     ((rowsum[b2][0][lane] + rowsum[b2][1][lane]) +
                      (rowsum[b2][2][lane] + rowsum[b2][3][lane])) -
                     colsum[b2][lane];
-    const float v = vs[b2][lane];
+    const float v = vs[b2][0][lane] + vs[b2][1][lane];
     float after = u, before = v;  // sums from the token on, and up to it
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
@@ -1042,123 +1064,135 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
   // The wave with least of K forms dla of the round before, and the one whose
   // loads are done first the running sums of the next.
   constexpr int kFinish = 3, kSums = 0;
-  Cum cum;
-  if (wave == kSums) cum = cumulate(lav);
   const uint32_t rounds = hn * sh.ptiles;
-  for (uint32_t k = 0; k < rounds; ++k) {
-    const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
-    const int p0 = pt * PT, rows = min(PT, P - p0), now = k & 1;
-    const int place = kTwice ? now : 0, at4 = k & 3;
-    T *xs = x_s[place], *dys = dy_s[place], *sr = s_s[kPlaces * place];
-    T* rr = s_s[kPlaces * place + kPlaces - 1];
-    float *hi = hi_s[now], *lo = lo_s[now], *ec = ec_s[now], *wt = wt_s[now];
-    if constexpr (!kTwice) __syncthreads();
-    xst.store(xs, XS);
-    dyst.store(dys, XS);
-    sst.store(sr, NS);
-    if constexpr (kTwice) rst.store(rr, NS);
-    if (wave == kSums) {
-      hi[lane] = cum.hi;
-      lo[lane] = cum.lo;
-      ec[lane] = cum.e;
-      wt[lane] = cum.w;
-      reset[at4][lane] = lav < kReset;
-      if (lane == 0) total[at4] = cum.total;
-    }
-    const float dot = sum_groups(sum16(rst.dot(sst)));
-    if (lane == 0) dots[at4][wave] = dot;
-    __syncthreads();
-    if (k + 1 < rounds) fetch_tokens(k + 1);
-    if (wave == kFinish && k) finish(k - 1);
-    Four dg[4];  // D G as an operand, summed over s
-    if (left) {
-      const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
-      float cols = 0.0f;
-      Frag xf[PT / 32];
-#pragma unroll
-      for (int q = 0; q < PT / 32; ++q)
-        xf[q] = row_frag(xs + (16 * tile + col) * XS + 32 * q + 8 * g);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f32x4 m = {0, 0, 0, 0}, e = {0, 0, 0, 0};
-        if (j >= tile) {
-#pragma unroll
-          for (int q = 0; q < PT / 32; ++q)
-            m = mma(row_frag(dys + (16 * j + col) * XS + 32 * q + 8 * g), xf[q], m);
-          const f32x4 hs = *reinterpret_cast<const f32x4*>(hi + 16 * j + 4 * g);
-          const f32x4 ls = *reinterpret_cast<const f32x4*>(lo + 16 * j + 4 * g);
-#pragma unroll
+  // Both kinds of waves run through the same rounds and barriers, each with the
+  // registers of its own part only.
+  auto run = [&](auto is_left) {
+    fetch_one(is_left, 0);
+    fetch_two(is_left, 0);
+    Cum cum;
+    if (is_left && wave == kSums) cum = cumulate(lav);
+    for (uint32_t k = 0; k < rounds; ++k) {
+      const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
+      const int p0 = pt * PT, rows = min(PT, P - p0), now = k & 1;
+      const int place = kTwice ? now : 0, at4 = k & 3;
+      T *xs = x_s[place], *dys = dy_s[place], *sr = s_s[kPlaces * place];
+      T* rr = s_s[kPlaces * place + kPlaces - 1];
+      float *hi = hi_s[now], *lo = lo_s[now], *ec = ec_s[now], *wt = wt_s[now];
+      if constexpr (!kTwice) __syncthreads();
+      if constexpr (is_left) {
+        staged(XStage{}, one).store(xs, XS);
+        staged(XStage{}, two).store(dys, XS);
+      } else {
+        staged(SStage{}, one).store(sr, NS);
+        if constexpr (kTwice) staged(SStage{}, two).store(rr, NS);
+        const float dot = sum_groups(sum16(staged(SStage{}, two).dot(staged(SStage{}, one))));
+        if (lane == 0) dots[at4][wave - 4] = dot;
+      }
+      if (is_left && wave == kSums) {
+        hi[lane] = cum.hi;
+        lo[lane] = cum.lo;
+        ec[lane] = cum.e;
+        wt[lane] = cum.w;
+        reset[at4][lane] = lav < kReset;
+        if (lane == 0) total[at4] = cum.total;
+      }
+      __syncthreads();
+      if (k + 1 < rounds) fetch_one(is_left, k + 1);
+      if (is_left && wave == kFinish && k) finish(k - 1);
+      Four dg[4];  // D G as an operand, summed over s
+      if constexpr (is_left) {
+        const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
+        float cols = 0.0f;
+        Frag xf[PT / 32];
+  #pragma unroll
+        for (int q = 0; q < PT / 32; ++q)
+          xf[q] = row_frag(xs + (16 * tile + col) * XS + 32 * q + 8 * g);
+  #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f32x4 m = {0, 0, 0, 0}, e = {0, 0, 0, 0};
+          if (j >= tile) {
+  #pragma unroll
+            for (int q = 0; q < PT / 32; ++q)
+              m = mma(row_frag(dys + (16 * j + col) * XS + 32 * q + 8 * g), xf[q], m);
+            const f32x4 hs = *reinterpret_cast<const f32x4*>(hi + 16 * j + 4 * g);
+            const f32x4 ls = *reinterpret_cast<const f32x4*>(lo + 16 * j + 4 * g);
+  #pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              e[i] = exp2_seen(j > tile || 4 * g + i >= col, hs[i], ls[i], hr, lr);
+              m[i] *= e[i];
+            }
+            wk[j] += m;
+            e *= gt[j];
+            m *= gt[j];
+          }
+          dg[j] = to_four<T>(e);
+          cols += (m[0] + m[1]) + (m[2] + m[3]);
+  #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            e[i] = exp2_seen(j > tile || 4 * g + i >= col, hs[i], ls[i], hr, lr);
-            m[i] *= e[i];
+            const float s = sum16(m[i]);
+            if (col == 0) rowsum[now][tile][16 * j + 4 * g + i] = s;
           }
-          wk[j] += m;
-          e *= gt[j];
-          m *= gt[j];
         }
-        dg[j] = to_four<T>(e);
-        cols += (m[0] + m[1]) + (m[2] + m[3]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float s = sum16(m[i]);
-          if (col == 0) rowsum[now][tile][16 * j + 4 * g + i] = s;
-        }
+        cols = sum_groups(cols);
+        if (g == 0) colsum[now][16 * tile + col] = cols;
+      } else {
+        sum_state(dc, sr, dys, cs, ec[16 * tile + col], us[now][half_of]);
       }
-      cols = sum_groups(cols);
-      if (g == 0) colsum[now][16 * tile + col] = cols;
-    } else {
-      sum_state(dc, sr, dys, cs, ec[16 * tile + col], us[now]);
-    }
-    if (k + 1 < rounds) fetch_state(k + 1);
-    if constexpr (!kTwice) {
-      __syncthreads();
-      rst.store(rr, NS);
-      __syncthreads();
-    }
-    if (k + 1 < rounds) fetch_adjoint(k + 1);
-    if (left) {
-      const float wr = wt[16 * tile + col];
-      Frag bf[NT / 32];
-#pragma unroll
-      for (int q = 0; q < NT / 32; ++q)
-        bf[q] = row_frag(bs + (16 * tile + col) * NS + 32 * q + 8 * g);
-      const Mem dx((T*)a.dx + (((uint64_t)b * sh.len + t0) * sh.heads + h) * P + p0);
-      const uint32_t at = (16 * tile + col) * sh.heads * P * (uint32_t)sizeof(T);
-#pragma unroll
-      for (int x = 0; x < PT / 16; x += 2) {
-        f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-        for (int q = 0; q < NT / 32; ++q) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            acc[e] = mma(row_frag(rr + (16 * (x + e) + col) * NS + 32 * q + 8 * g), bf[q], acc[e]);
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) acc[e] *= wr;
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          if (j + 1 >= tile) {
-#pragma unroll
+      if constexpr (!kTwice) {
+        __syncthreads();
+        if constexpr (!is_left) staged(SStage{}, two).store(rr, NS);
+        __syncthreads();
+      }
+      if (k + 1 < rounds) fetch_two(is_left, k + 1);
+      if constexpr (is_left) {
+        const float wr = wt[16 * tile + col];
+        Frag bf[NT / 32];
+  #pragma unroll
+        for (int q = 0; q < NT / 32; ++q)
+          bf[q] = row_frag(bs + (16 * tile + col) * NS + 32 * q + 8 * g);
+        const Mem dx((T*)a.dx + (((uint64_t)b * sh.len + t0) * sh.heads + h) * P + p0);
+        const uint32_t at = (16 * tile + col) * sh.heads * P * (uint32_t)sizeof(T);
+  #pragma unroll
+        for (int x = 0; x < PT / 16; x += 2) {
+          f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  #pragma unroll
+          for (int q = 0; q < NT / 32; ++q) {
+  #pragma unroll
             for (int e = 0; e < 2; ++e)
-              acc[e] = mma(join(col_four(dys, XS, 16 * j + 4 * g, 16 * (x + e)),
-                                col_four(dys, XS, 16 * j + 16 + 4 * g, 16 * (x + e))),
-                           join(dg[j], dg[j + 1]), acc[e]);
+              acc[e] = mma(row_frag(rr + (16 * (x + e) + col) * NS + 32 * q + 8 * g), bf[q], acc[e]);
+          }
+  #pragma unroll
+          for (int e = 0; e < 2; ++e) acc[e] *= wr;
+  #pragma unroll
+          for (int j = 0; j < 4; j += 2) {
+            if (j + 1 >= tile) {
+  #pragma unroll
+              for (int e = 0; e < 2; ++e)
+                acc[e] = mma(join(col_four(dys, XS, 16 * j + 4 * g, 16 * (x + e)),
+                                  col_four(dys, XS, 16 * j + 16 + 4 * g, 16 * (x + e))),
+                             join(dg[j], dg[j + 1]), acc[e]);
+            }
+          }
+  #pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int pp = 16 * (x + e) + 4 * g;
+            dx.store_four<T, VEC>(at + pp * (uint32_t)sizeof(T), acc[e],
+                                  16 * tile + col < n ? rows - pp : 0);
           }
         }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int pp = 16 * (x + e) + 4 * g;
-          dx.store_four<T, VEC>(at + pp * (uint32_t)sizeof(T), acc[e],
-                                16 * tile + col < n ? rows - pp : 0);
-        }
+      } else {
+        sum_state(db, rr, xs, bs, wt[16 * tile + col], vs[now][half_of]);
       }
-    } else {
-      sum_state(db, rr, xs, bs, wt[16 * tile + col], vs[now]);
+      if (is_left && wave == kSums && k + 1 < rounds) cum = cumulate(lav);
     }
-    if (wave == kSums && k + 1 < rounds) cum = cumulate(lav);
-  }
-  __syncthreads();
-  if (wave == kFinish) finish(rounds - 1);
+    __syncthreads();
+    if (is_left && wave == kFinish) finish(rounds - 1);
+  };
+  if (left)
+    run(std::true_type{});
+  else
+    run(std::false_type{});
   T* xs = x_s[0];
   // W to LDS (rows s, columns r), then its products with B and C
   if (left) {
@@ -1181,15 +1215,15 @@ __global__ __launch_bounds__(512) void k_scan_grad(ScanShape sh, ScanGrad a) {
                  col_four(xs, XS, 32 * q + 8 * g + 4, 16 * tile));
   }
 #pragma unroll
-  for (int x = 0; x < NT / 16; ++x) {
+  for (int x = 0; x < kOwn; ++x) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      dc[x] = mma(join(state_four(bs, NS, 32 * q + 8 * g, x),
-                       state_four(bs, NS, 32 * q + 8 * g + 4, x)), wc[q], dc[x]);
-      db[x] = mma(join(state_four(cs, NS, 32 * q + 8 * g, x),
-                       state_four(cs, NS, 32 * q + 8 * g + 4, x)), wb[q], db[x]);
+      dc[x] = mma(join(state_four(bs, NS, 32 * q + 8 * g, first + x),
+                       state_four(bs, NS, 32 * q + 8 * g + 4, first + x)), wc[q], dc[x]);
+      db[x] = mma(join(state_four(cs, NS, 32 * q + 8 * g, first + x),
+                       state_four(cs, NS, 32 * q + 8 * g + 4, first + x)), wb[q], db[x]);
     }
-    const int nn = state_col(x, g);
+    const int nn = state_col(first + x, g);
     const uint32_t at = (16 * tile + col) * sh.groups * N + nn;
     const int some = 16 * tile + col < n ? N - nn : 0;
     if (a.db_part) {
@@ -1336,7 +1370,7 @@ hipError_t launch_scan_out(uint32_t dtype, const ScanShape& sh, const ScanDir& d
 hipError_t launch_scan_grad(uint32_t dtype, const ScanShape& sh, const ScanGrad& g,
                             hipStream_t s) {
   const dim3 grid(sh.batch * sh.chunks, sh.groups * g.splits);
-#define CALL(T, NT, VEC) (k_scan_grad<T, NT, VEC><<<grid, 512, 0, s>>>(sh, g), hipGetLastError())
+#define CALL(T, NT, VEC) (k_scan_grad<T, NT, VEC><<<grid, kGradThreads, 0, s>>>(sh, g), hipGetLastError())
   hipError_t e = FESC_SCAN_CASES(dtype, sh, CALL);
 #undef CALL
   if (e || g.splits == 1) return e;

@@ -18,7 +18,7 @@ constexpr uint64_t kMaxStride = 1ull << 40;
 // A chunk's rows lie within 2^31 bytes of its first one.
 constexpr uint64_t kMaxTokenStride = 1ull << 22;
 // A launch counts its work items in 32 bits.
-constexpr uint64_t kMaxGrid256 = 1ull << 24, kMaxGrid512 = 1ull << 23;
+constexpr uint64_t kMaxGrid256 = 1ull << 24, kMaxGrid512 = 1ull << 23, kMaxGrid1024 = 1ull << 22;
 
 uint32_t elem_bytes(uint32_t dtype) { return dtype == FESC_BF16 ? 2 : 4; }
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -189,7 +189,7 @@ int check_grid(const ScanShape& s) {
   const uint64_t bh = (uint64_t)s.batch * s.heads;
   const uint64_t join = ((uint64_t)s.head_dim * s.d_state + 255) / 256;
   if (bh * s.ptiles * s.segs >= kMaxGrid512 || bh * join >= kMaxGrid256 ||
-      (uint64_t)s.batch * s.chunks >= kMaxGrid512 ||
+      (uint64_t)s.batch * s.chunks >= kMaxGrid1024 ||
       (uint64_t)s.batch * s.len * s.groups * s.d_state >= kMaxGrid256 * 256)
     return fail(FESC_ERR_ARG, "batch * len * heads too large for one call");
   return FESC_OK;

@@ -7,6 +7,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace fesc {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
@@ -103,6 +105,23 @@ __device__ __forceinline__ float sum16(float v) {
   v += dpp_move<0x141>(v);  // row_half_mirror
   v += dpp_move<0x140>(v);  // row_mirror
   return v;
+}
+// Sixteen such sums at once: lane l % 16 gets that of v[l % 16].  Each step
+// halves the values and hands the others to a lane that keeps them.
+__device__ __forceinline__ float sums16(float (&v)[16]) {
+  const int l = threadIdx.x & 15;
+  auto halve = [&](auto n, bool upper, auto move) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float a = v[i], b = v[i + n];
+      v[i] = (upper ? b : a) + move(upper ? a : b);
+    }
+  };
+  halve(std::integral_constant<int, 8>{}, l & 8, [](float x) { return dpp_move<0x140>(x); });
+  halve(std::integral_constant<int, 4>{}, l & 4, [](float x) { return dpp_move<0x141>(x); });
+  halve(std::integral_constant<int, 2>{}, l & 2, [](float x) { return dpp_move<0x4e>(x); });
+  halve(std::integral_constant<int, 1>{}, l & 1, [](float x) { return dpp_move<0xb1>(x); });
+  return v[0];
 }
 __device__ __forceinline__ float sum_groups(float v) {
   v += __shfl_xor(v, 16);

@@ -1061,9 +1061,9 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       dla = 0.0f;
     }
   };
-  // The wave with least of K forms dla of the round before, and the one whose
-  // loads are done first the running sums of the next.
-  constexpr int kFinish = 3, kSums = 0;
+  // One of the other waves, which have less to do, forms dla of the round before;
+  // the running sums of the next are left to the wave with least of K.
+  constexpr int kFinish = 4, kSums = 3;
   const uint32_t rounds = hn * sh.ptiles;
   // Both kinds of waves run through the same rounds and barriers, each with the
   // registers of its own part only.
@@ -1099,11 +1099,11 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       }
       __syncthreads();
       if (k + 1 < rounds) fetch_one(is_left, k + 1);
-      if (is_left && wave == kFinish && k) finish(k - 1);
+      if (!is_left && wave == kFinish && k) finish(k - 1);
       Four dg[4];  // D G as an operand, summed over s
       if constexpr (is_left) {
         const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
-        float cols = 0.0f;
+        float cols = 0.0f, rows16[16];  // of the tokens 16 j + 4 g + i
         Frag xf[PT / 32];
   #pragma unroll
         for (int q = 0; q < PT / 32; ++q)
@@ -1129,11 +1129,9 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
           dg[j] = to_four<T>(e);
           cols += (m[0] + m[1]) + (m[2] + m[3]);
   #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float s = sum16(m[i]);
-            if (col == 0) rowsum[now][tile][16 * j + 4 * g + i] = s;
-          }
+          for (int i = 0; i < 4; ++i) rows16[4 * j + i] = m[i];
         }
+        rowsum[now][tile][16 * (col >> 2) + 4 * g + (col & 3)] = sums16(rows16);
         cols = sum_groups(cols);
         if (g == 0) colsum[now][16 * tile + col] = cols;
       } else {
@@ -1187,7 +1185,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       if (is_left && wave == kSums && k + 1 < rounds) cum = cumulate(lav);
     }
     __syncthreads();
-    if (is_left && wave == kFinish) finish(rounds - 1);
+    if (!is_left && wave == kFinish) finish(rounds - 1);
   };
   if (left)
     run(std::true_type{});

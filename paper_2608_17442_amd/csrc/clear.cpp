@@ -85,16 +85,19 @@ struct Rows {
 //    144 x 128         306        -          262         216
 //    192 x 128         333        -          365         299
 //     24 x 782           -      275            -         242
-// The gradient's pass carries states in both directions, so that a cut doubles its
-// work (whole gradient call, tiles of both directions):
-//     48 x 32           77       59           62          68
-//     96 x 32           89       94           84          92
-//    144 x 32          112        -          118         128
-//    192 x 32          115        -          139         135
-//     48 x 128         244      147          134         142
-//     48 x 256         516      304          266         257
+// The gradient's pass carries states only, in both directions, so that a cut doubles
+// its work; of its workgroups 384 tiles' fit at once (whole gradient call, tiles of
+// both directions, segments in brackets):
+//     48 x 32           69       55 (5)      55 (8)
+//     72 x 64          127      114 (3)     105 (4)
+//     96 x 16           49        -          52 (4)
+//     96 x 32           77       85 (2)      74 (4)
+//    144 x 32           93        -         107 (3)
+//     48 x 128         215      132 (5)     122 (8)
+//     48 x 256         470      275 (5)     250 (8)
 constexpr uint64_t kUnits = 256;
 constexpr uint64_t kWholeTiles = 171, kWholeTilesGrad = 96;  // whole from here on
+constexpr uint64_t kGradTiles = 384;
 constexpr uint64_t kTwoChunks = 2 * kUnits * 6;      // tiles * chunks for two a unit
 constexpr uint64_t kPairChunks = 8192;               // tiles * chunks for pairs
 constexpr uint64_t kPairTiles = 256;
@@ -119,17 +122,20 @@ ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   const bool pairs = d->dtype == FESC_BF16 && d->heads / d->groups * s.ptiles % 2 == 0;
   uint64_t segs = 1;
   s.tiles = 1;
-  const uint64_t whole = dirs == 1 ? kWholeTiles : kWholeTilesGrad;
   const uint64_t work = tiles * s.chunks;
-  if (tiles && pairs && tiles < (dirs == 1 ? kPairTiles : whole) && work >= kPairChunks) {
+  if (tiles && dirs == 2) {
+    if (tiles < kWholeTilesGrad)
+      segs = std::min<uint64_t>((d->dtype == FESC_BF16 ? kGradTiles : kUnits) / tiles, s.chunks / 4);
+  } else if (tiles && pairs && tiles < kPairTiles && work >= kPairChunks) {
     s.tiles = 2;
     segs = 2 * kUnits / (tiles / 2);
-  } else if (tiles && tiles < whole) {
+  } else if (tiles && tiles < kWholeTiles) {
     if (d->dtype == FESC_BF16 && work >= kTwoChunks)
       segs = 2 * kUnits / tiles;
     else
-      segs = std::max<uint64_t>(1, std::min<uint64_t>(kUnits / tiles, s.chunks / 2));
+      segs = std::min<uint64_t>(kUnits / tiles, s.chunks / 2);
   }
+  segs = std::max<uint64_t>(1, segs);
   s.seg_chunks = (uint32_t)((s.chunks + segs - 1) / segs);
   s.segs = s.chunks ? (s.chunks + s.seg_chunks - 1) / s.seg_chunks : 1;
   s.joined = s.segs > kJoinedSegs;

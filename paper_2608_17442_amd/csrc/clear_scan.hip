@@ -511,9 +511,10 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[HB][OWN],
 // zero, and its total decay, to seg_states and seg_decay.  Otherwise from the
 // state that enters the segment: the states that enter the chunks, and the
 // final state.  Chunks lie in LDS in turn in two places: one barrier each.
+// blockIdx.y: the NT entries of the state at hand.
 template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
-__global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_scan_states(
-    ScanShape sh, ScanDir d0, ScanDir d1, bool summaries) {
+__global__ __launch_bounds__(256 * EW, HB * EW == 1 ? 3 : (sizeof(T) == 2 ? 2 : 1) * EW)
+    void k_scan_states(ScanShape sh, ScanDir d0, ScanDir d1, bool summaries) {
   using Tiles = ScanTiles<T, NT, HB, EW>;
   constexpr int kThreads = Tiles::kThreads;
   constexpr int XS = Tiles::XS, NS = Tiles::NS;
@@ -527,13 +528,14 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
   const int lane = threadIdx.x & 63;
   const int sums_of = sums_tile<HB, EW>();  // whose running sums this wave forms
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + (lane & 15);
+  const int n0 = blockIdx.y * NT, m0 = t0 + n0 / 16;  // first entry and tile in the state
   // segments and chunks are counted in the direction of the pass
   const int first = at.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
   if (summaries && at.seg + 1 == sh.segs) return;  // no segment follows the last
   const uint64_t size = (uint64_t)P * N;
   const T* u = (const T*)d.u + at.b * d.u_batch;
-  const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
+  const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N + n0;
   const T* la = (const T*)sh.la + at.b * sh.la_batch + Head(sh, at, sums_of < 0 ? 0 : sums_of).h;
 
   f32x4 s[HB][Tiles::kOwn];
@@ -544,14 +546,14 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
 #pragma unroll
       for (int t = 0; t < Tiles::kOwn; ++t) s[h][t] = f32x4{0, 0, 0, 0};
     } else {
-      enter_segment<VEC>(s[h], sh, d, hd.at, at.seg, hd.p0, p, hd.rows, t0);
+      enter_segment<VEC>(s[h], sh, d, hd.at, at.seg, hd.p0, p, hd.rows, m0);
     }
   }
   using XStage = Stage<T, Q, PT, kThreads, VEC>;
   using NStage = Stage<T, Q, NT, kThreads, VEC>;
   XStage xst[HB];
   NStage bst;
-  const typename NStage::In bin(d.v_token, N);
+  const typename NStage::In bin(d.v_token, min(NT, N - n0));
   float lav = 0.0f;  // log decay of token `lane` of that tile
   const uint32_t la_at = lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T);
   auto chunk = [&](int k) { return d.reverse ? (int)sh.chunks - 1 - (first + k) : first + k; };
@@ -591,7 +593,7 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
       for (int h = 0; h < HB; ++h) {
         const Head hd(sh, at, h);
         store_state<VEC>(s[h], (T*)d.chunk_states + (hd.at * sh.chunks + chunk(k)) * size +
-                                   (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
+                                   (uint64_t)hd.p0 * N, p, hd.rows, N, m0);
       }
     }
     typename Elem<T>::Frag xf[HB][2];
@@ -610,10 +612,11 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_sca
     const uint64_t tile = (uint64_t)hd.p0 * N;
     if (summaries) {
       store_state<VEC>(s[h], d.seg_states + (hd.at * sh.segs + at.seg + 1) * size + tile, p,
-                       hd.rows, N, t0);
-      if (threadIdx.x == 0 && hd.p0 == 0) d.seg_decay[hd.at * sh.segs + at.seg] = decay[h];
+                       hd.rows, N, m0);
+      if (threadIdx.x == 0 && hd.p0 == 0 && n0 == 0)
+        d.seg_decay[hd.at * sh.segs + at.seg] = decay[h];
     } else if (d.fin && at.seg + 1 == sh.segs) {
-      store_state<VEC>(s[h], d.fin + hd.at * size + tile, p, hd.rows, N, t0);
+      store_state<VEC>(s[h], d.fin + hd.at * size + tile, p, hd.rows, N, m0);
     }
   }
 }
@@ -1300,7 +1303,7 @@ __global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to
 template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipStream_t s) {
   const ScanDir &d0 = d[0], &d1 = d[nd - 1];
-  const dim3 grid(sh.batch * sh.segs * (sh.heads * sh.ptiles / HB), 1, nd);
+  const dim3 grid(sh.batch * sh.segs * (sh.heads * sh.ptiles / HB), (sh.d_state + NT - 1) / NT, nd);
   if (sh.segs > 1) {
     k_scan_states<T, NT, VEC, PARTS, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, true);
     if (hipError_t e = hipGetLastError()) return e;
@@ -1332,6 +1335,12 @@ hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipS
 template <typename T, int NT, bool VEC>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, hipStream_t s) {
 #define FORM(PARTS, HB, EW) (states<T, NT, VEC, PARTS, HB, EW>(sh, d, nd, true, s))
+  // Without outputs the two halves of a long state's entries need nothing of each
+  // other: workgroups of four waves, three on a compute unit.  384 tiles of 32 chunks,
+  // 200 MB of states: 96 us, with eight waves for the whole state 109.
+  if constexpr (sizeof(T) == 2 && VEC && NT == 128)
+    return sh.exact ? states<T, 64, VEC, 3, 1, 1>(sh, d, nd, true, s)
+                    : states<T, 64, VEC, 2, 1, 1>(sh, d, nd, true, s);
   FESC_SCAN_FORMS(FORM);
 #undef FORM
 }

@@ -633,10 +633,20 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
   const float* decay = d.seg_decay + head * sh.segs;
   float carry = d.init ? d.init[head * size + e] : 0.0f;
   s[0] = carry;
-  for (uint32_t j = 1; j < sh.segs; ++j) {
-    float* at = s + (uint64_t)j * size;
-    carry = __builtin_fmaf(decay[j - 1], carry, *at);
-    *at = carry;
+  constexpr uint32_t kAtOnce = 8;  // loads under way
+  for (uint32_t j0 = 1; j0 < sh.segs; j0 += kAtOnce) {
+    float own[kAtOnce], keep[kAtOnce];
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      const uint32_t j = min(j0 + k, sh.segs - 1);
+      own[k] = s[(uint64_t)j * size];
+      keep[k] = decay[j - 1];
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      carry = __builtin_fmaf(keep[k], carry, own[k]);
+      if (j0 + k < sh.segs) s[(uint64_t)(j0 + k) * size] = carry;
+    }
   }
 }
 

@@ -176,6 +176,40 @@ struct Rows {
   }
 };
 
+// One unit of 16 bytes, as loaded.  Rows at any alignment: the 16 bytes from the
+// word on in which the unit begins and the word behind them, or, of a row's last
+// unit, of its last 16 bytes, so that every word read holds an element of the row;
+// `by`: how many elements it lies too far up.
+template <bool VEC>
+struct Loaded {
+  u32x4 w;
+};
+template <>
+struct Loaded<false> {
+  u32x4 w;
+  uint32_t more, by;
+};
+template <typename T>
+__device__ __forceinline__ u32x4 settled(const Loaded<true>& l) {
+  return l.w;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 settled(const Loaded<false>& l) {
+  uint32_t v[8] = {l.w[0], l.w[1], l.w[2], l.w[3], 0, 0, 0, 0};
+  if constexpr (sizeof(T) == 2) v[4] = l.more & 0xffffu;
+  const uint32_t words = sizeof(T) == 2 ? l.by >> 1 : l.by;
+#pragma unroll
+  for (int d = 4; d >= 1; d /= 2) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) v[i] = words & d ? (i + d < 5 ? v[i + d] : 0) : v[i];
+  }
+  u32x4 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    o[i] = sizeof(T) == 2 ? __builtin_amdgcn_alignbyte(v[i + 1], v[i], (l.by & 1) * 2) : v[i];
+  return o;
+}
+
 // Registers of one thread for a tile of ROWS x COLS elements on its way from
 // global memory to LDS; rows and columns past the valid ones are zero.
 template <typename T, int ROWS, int COLS, int THREADS, bool VEC, int FIRST = 0>
@@ -185,14 +219,14 @@ struct Stage {
   static constexpr int kUnits = ROWS * kPerRow / THREADS;
   static_assert(ROWS * kPerRow % THREADS == 0, "whole units per thread");
   using In = Rows<T, COLS, THREADS, VEC, FIRST>;
-  u32x4 r[kUnits];
+  Loaded<VEC> r[kUnits];
 
   __device__ __forceinline__ void load(const T* base, const In& in, int rows) {
     if constexpr (VEC) {
       const Mem m(base, in.bytes(rows));
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) r[k] = m.load16(in.first, k * in.step);
-    } else {
+      for (int k = 0; k < kUnits; ++k) r[k].w = m.load16(in.first, k * in.step);
+    } else if (in.cols < kUnit) {  // rows of a few elements: one at a time
       const Mem m(base);
 #pragma unroll
       for (int k = 0; k < kUnits; ++k) {
@@ -209,7 +243,22 @@ struct Stage {
           else
             v[j / 2] |= w << (16 * (j & 1));
         }
-        r[k] = v;
+        r[k] = {v, 0, 0};
+      }
+    } else {
+      const uint32_t off = reinterpret_cast<uintptr_t>(base) & 3;
+      const Mem m(reinterpret_cast<const char*>(base) - off);
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) {
+        const int i = (threadIdx.x - FIRST) + k * THREADS;
+        const int row = i / kPerRow, col = i % kPerRow * kUnit;
+        const int from = min(col, in.cols - kUnit);
+        const uint32_t at = off + (row * in.pitch + from) * (uint32_t)sizeof(T);
+        const bool seen = row < rows && col < in.cols;
+        const uint32_t odd = sizeof(T) == 2 ? at >> 1 & 1 : 0;
+        r[k].w = m.load16(seen ? at & ~3u : kAbsent);
+        r[k].more = sizeof(T) == 2 ? m.load_bits<float>(seen && odd ? (at & ~3u) + 16 : kAbsent) : 0;
+        r[k].by = col - from + odd;
       }
     }
   }
@@ -217,21 +266,21 @@ struct Stage {
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
       const int i = (threadIdx.x - FIRST) + k * THREADS;
-      *reinterpret_cast<u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit) = r[k];
+      *reinterpret_cast<u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit) = settled<T>(r[k]);
     }
   }
   __device__ __forceinline__ void take(const T* tile, int pitch) {
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
       const int i = (threadIdx.x - FIRST) + k * THREADS;
-      r[k] = *reinterpret_cast<const u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit);
+      r[k].w = *reinterpret_cast<const u32x4*>(tile + i / kPerRow * pitch + i % kPerRow * kUnit);
     }
   }
   __device__ __forceinline__ void put(T* base, const In& out, int rows) const {
     if constexpr (VEC) {
       const Mem m(base, out.bytes(rows));
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) m.store16(out.first, r[k], k * out.step);
+      for (int k = 0; k < kUnits; ++k) m.store16(out.first, r[k].w, k * out.step);
     } else {
       const Mem m(base);
 #pragma unroll
@@ -242,8 +291,9 @@ struct Stage {
 #pragma unroll
         for (int j = 0; j < kUnit; ++j)
           m.store_bits<T>(row < rows && col + j < out.cols ? at + j * (uint32_t)sizeof(T) : kAbsent,
-                          sizeof(T) == 4 ? r[k][j * sizeof(T) / 4]
-                                         : r[k][j * sizeof(T) / 4] >> (16 * (j & 1)) & 0xffffu);
+                          sizeof(T) == 4
+                              ? r[k].w[j * sizeof(T) / 4]
+                              : r[k].w[j * sizeof(T) / 4] >> (16 * (j & 1)) & 0xffffu);
       }
     }
   }
@@ -252,9 +302,10 @@ struct Stage {
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
+      const u32x4 a = settled<T>(r[k]), b = settled<T>(o.r[k]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t v = r[k][j], w = o.r[k][j];
+        const uint32_t v = a[j], w = b[j];
         if constexpr (sizeof(T) == 4) {
           s = __builtin_fmaf(__uint_as_float(v), __uint_as_float(w), s);
         } else {
@@ -938,7 +989,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   using XStage = Stage<T, Q, PT, 256, VEC>;
   using SStage = Stage<T, PT, NT, 512, VEC, 256>;
   constexpr int kUnits = XStage::kUnits > SStage::kUnits ? XStage::kUnits : SStage::kUnits;
-  u32x4 one[kUnits], two[kUnits];
+  Loaded<VEC> one[kUnits], two[kUnits];
   if (!left) {
     using NStage = Stage<T, Q, NT, 512, VEC, 256>;
     NStage st, st2;
@@ -954,7 +1005,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent;
   // the loads of round k (head of the split and channel tile): la, x and S, then
   // dy and R
-  auto tokens = [&](const void* base, uint64_t batch, uint64_t token, uint32_t k, u32x4* r) {
+  auto tokens = [&](const void* base, uint64_t batch, uint64_t token, uint32_t k, Loaded<VEC>* r) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
     XStage st;
     st.load((const T*)base + b * batch + t0 * token + (int64_t)h * P + pt * PT,
@@ -962,7 +1013,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
 #pragma unroll
     for (int u = 0; u < XStage::kUnits; ++u) r[u] = st.r[u];
   };
-  auto states = [&](const void* base, uint32_t k, u32x4* r) {
+  auto states = [&](const void* base, uint32_t k, Loaded<VEC>* r) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
     SStage st;
     st.load((const T*)base + (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size +
@@ -986,7 +1037,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
     else
       states(a.r_in, k, two);
   };
-  auto staged = [](auto st, const u32x4* r) {
+  auto staged = [](auto st, const Loaded<VEC>* r) {
 #pragma unroll
     for (int u = 0; u < decltype(st)::kUnits; ++u) st.r[u] = r[u];
     return st;
@@ -1262,8 +1313,9 @@ __global__ __launch_bounds__(256) void k_scan_parts(ScanGrad a, uint64_t count) 
 
 // One served token per row: S = e^{la} S + x B^T in place, y = S C.  Memory
 // bound by the state, which is read and written once: 250 rows of 24 heads of
-// 64 x 128 in 59.5 us, 6.6 TB/s with the state still in the memory-side cache, 79 us as a call on other states.  LPR lanes share one state row, four entries each, so that
-// loads and stores are whole lines.
+// 64 x 128 in 59.5 us (6.6 TB/s) with part of the states still in the memory-side
+// cache, 79 us a call (5 TB/s, a copy's rate) where they are not.  LPR lanes share
+// one state row, four entries each, so that loads and stores are whole lines.
 template <typename T, int LPR, bool VEC>
 __global__ __launch_bounds__(256) void k_scan_step(StepArgs a, uint32_t psplit) {
   constexpr int kRows = 256 / LPR;  // state rows per pass of the workgroup

@@ -281,19 +281,25 @@ struct Stage {
       const Mem m(base, out.bytes(rows));
 #pragma unroll
       for (int k = 0; k < kUnits; ++k) m.store16(out.first, r[k].w, k * out.step);
-    } else {
-      const Mem m(base);
+    } else {  // whole units word by word, at any alignment of elements
+      const uint32_t off = reinterpret_cast<uintptr_t>(base) & 3;
+      const Mem m(reinterpret_cast<char*>(base) - off);
 #pragma unroll
       for (int k = 0; k < kUnits; ++k) {
         const int i = (threadIdx.x - FIRST) + k * THREADS;
         const int row = i / kPerRow, col = i % kPerRow * kUnit;
-        const uint32_t at = (row * out.pitch + col) * (uint32_t)sizeof(T);
+        const int left = row < rows ? out.cols - col : 0;
+        const uint32_t at = off + (row * out.pitch + col) * (uint32_t)sizeof(T);
+        const u32x4 v = r[k].w;
+        const bool odd = sizeof(T) == 2 && (at & 2);
+        m.store16(left >= kUnit && !odd ? at : kAbsent, v);
+        if (left < kUnit || odd) {
 #pragma unroll
-        for (int j = 0; j < kUnit; ++j)
-          m.store_bits<T>(row < rows && col + j < out.cols ? at + j * (uint32_t)sizeof(T) : kAbsent,
-                          sizeof(T) == 4
-                              ? r[k].w[j * sizeof(T) / 4]
-                              : r[k].w[j * sizeof(T) / 4] >> (16 * (j & 1)) & 0xffffu);
+          for (int j = 0; j < kUnit; ++j)
+            m.store_bits<T>(j < left ? at + j * (uint32_t)sizeof(T) : kAbsent,
+                            sizeof(T) == 4 ? v[j * sizeof(T) / 4]
+                                           : v[j * sizeof(T) / 4] >> (16 * (j & 1)) & 0xffffu);
+        }
       }
     }
   }

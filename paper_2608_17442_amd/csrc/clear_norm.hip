@@ -9,6 +9,9 @@
 // by memory: each array passes once, a row staying in the registers of the
 // lanes that share it, for the gradient too (v is formed again from its
 // inputs rather than kept).
+// 16384 rows of 1536 in bfloat16, gated: 31 us (201 MB, 6.5 TB/s, in part from the
+// memory-side cache), gradient 58 + 4 us (352 MB, 5.7 TB/s); of 768, residual: 17 us,
+// gradient 25 + 4.
 #include <type_traits>
 
 #include "clear.hpp"

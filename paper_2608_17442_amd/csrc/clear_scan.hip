@@ -385,10 +385,12 @@ __device__ __forceinline__ Cum cumulate(float la) {
 // tiles t = e kOwn ... (e + 1) kOwn - 1 with n = state_col(t, g) + i (g = l / 16):
 // tiles 2 q and 2 q + 1 together are, in registers, the operand
 // S[p][32 q + 8 g ...] of the product with C.
-// The registers are held to two workgroups on a compute unit (in bfloat16: LDS
-// has no room for a second one in float32).
+// The registers are held to two workgroups on a compute unit: in bfloat16, as LDS
+// has no room for a second one in float32, and of the output kernel on aligned rows,
+// as others take more (13 x 1827 tokens, 20 heads of 100: 563 us at two, 364 at one).
 // HB = 2, EW = 1 moves the least through LDS per head; HB = 1, EW = 2 takes the
-// least time from one chunk to the next.
+// least time from one chunk to the next (2.6 us with outputs, one workgroup a unit;
+// EW = 1 3.0, EW = 4 2.8).
 template <typename T, int NT, int HB, int EW>
 struct ScanTiles {
   static constexpr int XS = PT + Elem<T>::kPad;
@@ -679,7 +681,8 @@ __global__ __launch_bounds__(256 * EW, HB * EW == 1 ? 3 : (sizeof(T) == 2 ? 2 : 
 }
 
 // Segment summaries to the states that enter the segments, in place: the
-// summary of segment j lies in the place of segment j + 1.
+// summary of segment j lies in the place of segment j + 1.  Bound by memory: 66 MB
+// (24 heads, 42 segments) in 12 us.
 __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, ScanDir d1) {
   const ScanDir& d = blockIdx.z ? d1 : d0;
   const uint32_t size = sh.head_dim * sh.d_state, blocks = (size + 255) / 256;
@@ -712,8 +715,11 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
 // EW = 2), and writes their products with each tile's decays to LDS; meanwhile the
 // state's part of y^T for its 16 channels and all tokens (half e), and its part
 // of the new state; then the chunk's own part of y^T from what all waves wrote.
+// Bound by the way from barrier to barrier, on which LDS, the matrix pipe and the
+// issue of instructions take turns: 8 x 2048 tokens, 24 heads of 64, state 128, 84 us
+// (25 at a copy's rate); 50001 tokens in segments of pairs 65 + 12 + 137 us (68).
 template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
-__global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 ? 2 : 1) * EW) void k_scan_out(
+__global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 && VEC ? 2 : 1) * EW) void k_scan_out(
     ScanShape sh, ScanDir d, ScanOut o) {
   using Tiles = ScanTiles<T, NT, HB, EW>;
   constexpr int kThreads = Tiles::kThreads;
@@ -957,7 +963,8 @@ constexpr int kGradThreads = 768;
 // The first sum of dla falls from t to t + 1 by row sum minus column sum of
 // D K G at t.  Wave w of 0..3 holds the columns r = 16 w ... of G, K and W
 // and forms dx; wave 4 + 4 e + w holds half e of the entries of dC and dB for the
-// tokens 16 w ....
+// tokens 16 w ....  8 x 2048 tokens, 24 heads: 87 us for 350 MB, 4 TB/s (its loads alone
+// 77); eight waves with one barrier a round 102, with four 120.
 template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGrad a) {
   constexpr int XS = PT + Elem<T>::kPad, NS = NT + Elem<T>::kPad;

@@ -34,7 +34,8 @@ struct Mem {
   // bytes: what lies behind them is absent too
   __device__ __forceinline__ explicit Mem(const void* base, uint32_t bytes = 0x7fffffff)
       : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000)) {}
-  // `more`: a part of the offset that is the same for the wave
+  // `more`: a part of the offset that is the same for the wave; the check against
+  // `bytes` counts it, also where it lies past them by itself
   __device__ __forceinline__ u32x4 load16(uint32_t at, uint32_t more = 0) const {
     return __builtin_amdgcn_raw_buffer_load_b128(r, at, more, 0);
   }

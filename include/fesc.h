@@ -794,7 +794,10 @@ typedef struct fesc_clear_scan_desc {
 /* Bytes of workspace of the forward (backward = 0) or backward call. */
 int fesc_clear_scan_workspace(const fesc_clear_scan_desc* desc, int backward, size_t* bytes);
 
-/* y and, unless NULL, the final state hT.  h0 may be NULL (zero). */
+/* y and, unless NULL, the final state hT.  h0 may be NULL (zero).  bfloat16 outputs are
+ * computed in 32 bits, or in operands within 2^-18 of them, and rounded once.  Where hT is
+ * wanted the weighted inputs of the states enter exactly instead of to within 2^-18: y then
+ * agrees with that of a call without hT to that, not bit for bit. */
 int fesc_clear_scan(const fesc_clear_scan_desc* desc, const void* x, const void* la, const void* B,
                     const void* C, const float* h0, void* y, float* hT, void* workspace,
                     size_t workspace_bytes, void* stream);

@@ -246,6 +246,8 @@ def scan(x, la, B, C, h0=None, return_state=False, stream=None):
     -inf resets the state), B and C [batch, len, groups, d_state]; the first
     two dimensions may have any strides, so slices of a wider projection do.
     h0 and the returned state: float32 [batch, heads, head_dim, d_state].
+    In bfloat16 y is rounded once; with `return_state` the states behind it are
+    held to 2^-24 instead of 2^-18, so it need not be the same to the last bit.
     Differentiable (once) with respect to all five.
     """
     if stream is not None:

@@ -69,8 +69,8 @@ struct Rows {
 //  - Otherwise segments of whole chunks; the price is a pass before, in which x and
 //    B are read for the segments' own states, and their join.  Two workgroups a
 //    unit where segments of six chunks remain, else one, two chunks at least.
-//  - Long sequences: segments in workgroups of two tiles (four waves), which
-//    share what is read of B and C and the product of the two.
+//  - Long sequences: two a unit, and the pass before in workgroups of two tiles (four
+//    waves), which share what is read of B.
 // Measured with 24 heads of 64, state 128, bfloat16, in us, forward:
 //    tiles x chunks   whole   one a unit   two a unit   pairs
 //     24 x 32           79       33            -          59

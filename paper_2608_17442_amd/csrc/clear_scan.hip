@@ -9,12 +9,12 @@
 //   S'  = e^{cum_Q} S + sum_r e^{cum_Q - cum_r} x_r B_r^T
 //
 // so the work is matrix products over 64 x 64 x N tiles (MFMA), and the state
-// stays in registers, in fp32, from chunk to chunk.  Products with the state
-// and with the matrix of decays take these operands rounded to the call's
-// type (one rounding on each path to an output, as large as that of the
-// output itself); the state's own update does not add to that: the weighted
-// inputs enter as bf16 parts, three that sum to the fp32 value exactly where the
-// state (or its gradient) is an output of the call, otherwise two.
+// stays in registers, in fp32, from chunk to chunk.  In bfloat16 the matrix instructions
+// take eight bits of an operand.  Operands that are not inputs (the state, the weighted
+// products C_s . B_r, the weighted inputs) enter as parts: two, within 2^-18 of the fp32
+// value, so that an output is rounded once, when it is stored; the weighted inputs of a
+// state (or of its gradient) that is an output of the call in three, which sum to the fp32
+// value exactly.
 #include <algorithm>
 #include <type_traits>
 
@@ -115,7 +115,7 @@ __device__ __forceinline__ f32x4 widen(const f32x4& v) { return v; }
 
 // The parts of a fp32 operand in the call's type: itself, or COUNT bf16 values.
 // Three, each the leading 8 bits of what the ones before leave, sum to it
-// exactly; two, each rounded to nearest, to within 2^-17 of it.
+// exactly; two, each rounded to nearest, to within 2^-18 of it.
 template <typename T, int COUNT>
 struct Parts;
 template <int COUNT>
@@ -387,10 +387,7 @@ __device__ __forceinline__ Cum cumulate(float la) {
 // S[p][32 q + 8 g ...] of the product with C.
 // The registers are held to two workgroups on a compute unit: in bfloat16, as LDS
 // has no room for a second one in float32, and of the output kernel on aligned rows,
-// as others take more (13 x 1827 tokens, 20 heads of 100: 563 us at two, 364 at one).
-// HB = 2, EW = 1 moves the least through LDS per head; HB = 1, EW = 2 takes the
-// least time from one chunk to the next (2.6 us with outputs, one workgroup a unit;
-// EW = 1 3.0, EW = 4 2.8).
+// as others take more.
 template <typename T, int NT, int HB, int EW>
 struct ScanTiles {
   static constexpr int XS = PT + Elem<T>::kPad;
@@ -710,53 +707,58 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
   }
 }
 
-// Outputs and final state.  Per chunk: wave 4 e + w forms the columns of token
-// tile w of G^T, G = C B^T, once for the HB tiles (the tokens r of half e where
-// EW = 2), and writes their products with each tile's decays to LDS; meanwhile the
-// state's part of y^T for its 16 channels and all tokens (half e), and its part
-// of the new state; then the chunk's own part of y^T from what all waves wrote.
+// Outputs and final state.  Per chunk: wave 4 e + w forms, for the tokens of tile w,
+// the columns of G^T, G = C B^T, of the tokens r of half e, and writes their products
+// with the decays to LDS; meanwhile, from its part of the state, a part of y^T for its 16
+// channels and all tokens, of which it hands the tokens of half 1 - e to the other
+// wave with these channels; and its part of the new state.  Then, for the tokens of half e,
+// the chunk's own part of y^T from what all waves wrote.
 // Bound by the way from barrier to barrier, on which LDS, the matrix pipe and the
 // issue of instructions take turns: 8 x 2048 tokens, 24 heads of 64, state 128, 84 us
-// (25 at a copy's rate); 50001 tokens in segments of pairs 65 + 12 + 137 us (68).
-template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
-__global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 && VEC ? 2 : 1) * EW) void k_scan_out(
-    ScanShape sh, ScanDir d, ScanOut o) {
-  using Tiles = ScanTiles<T, NT, HB, EW>;
-  constexpr int kThreads = Tiles::kThreads;
+// (25 at a copy's rate); 50001 tokens in segments 75 + 8 + 165 us (68).  Of these the second
+// parts of the operands cost some 8 and 35 us.
+template <typename T, int NT, bool VEC, int PARTS>
+__global__ __launch_bounds__(512, sizeof(T) == 2 && VEC ? 4 : 2) void k_scan_out(ScanShape sh,
+                                                                                 ScanDir d,
+                                                                                 ScanOut o) {
+  constexpr int EW = 2;
+  using Tiles = ScanTiles<T, NT, 1, EW>;
+  constexpr int kThreads = Tiles::kThreads, kOwn = Tiles::kOwn;
   constexpr int XS = Tiles::XS, NS = Tiles::NS;
-  constexpr int NQ = NT / 32, kTokenTiles = 4 / EW;
-  __shared__ __align__(16) T xs[HB][Q * XS];
+  constexpr int NQ = NT / 32;
+  using Frag = typename Elem<T>::Frag;
+  using Two = Parts<T, 2>;
+  constexpr int kParts = Two::kCount;
+  // The weighted products: rows s of 32 or, in the second half, 64 tokens r.
+  constexpr int kRow = 16 / sizeof(T), LS0 = 32 + kRow, LS1 = 64 + kRow, kLg = 32 * (LS0 + LS1);
+  __shared__ __align__(16) T xs[Q * XS];
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
-  __shared__ __align__(16) T lg[HB][Q * XS];
-  // the state's operands, lane by lane, where a wave holds only some of them
-  __shared__ __align__(16) T ss[EW > 1 ? HB * NQ : 1][EW > 1 ? PT * 32 : 8];
-  __shared__ __align__(16) float hi[2][HB][Q], lo[2][HB][Q], wt[2][HB][Q];
-  __shared__ float total[2][HB];
-  using Frag = typename Elem<T>::Frag;
-  const Where at = Where::of<HB>(sh);
-  const int sums_of = sums_tile<HB, EW>();
-  const int wave = wave_id() & 3, part = wave_id() >> 2, t0 = part * Tiles::kOwn;
+  __shared__ __align__(16) T lg[kParts][kLg];
+  __shared__ __align__(16) f32x4 ex[2][8][64];  // what is handed over, by lanes
+  __shared__ __align__(16) float hi[2][Q], lo[2][Q], wt[2][1][Q];
+  __shared__ float total[2][1];
+  const Where where = Where::of<1>(sh);
+  const Head at(sh, where, 0);
+  const int wave = wave_id() & 3, part = wave_id() >> 2, t0 = part * kOwn;
   const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const bool sums_here = wave_id() == 4;  // of the waves with least to do with G
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + col;
-  const int first = at.seg * sh.seg_chunks;
+  const int first = where.seg * sh.seg_chunks;
   const int count = min((int)sh.seg_chunks, (int)sh.chunks - first);
   const uint64_t size = (uint64_t)P * N;
-  const T* u = (const T*)d.u + at.b * d.u_batch;
-  const T* v = (const T*)d.v + at.b * d.v_batch + (int64_t)at.g * N;
-  const T* cc = (const T*)o.c + at.b * o.c_batch + (int64_t)at.g * N;
-  const T* la = (const T*)sh.la + at.b * sh.la_batch + Head(sh, at, sums_of < 0 ? 0 : sums_of).h;
+  const T* u = (const T*)d.u + where.b * d.u_batch + (int64_t)at.h * P + at.p0;
+  const T* v = (const T*)d.v + where.b * d.v_batch + (int64_t)where.g * N;
+  const T* cc = (const T*)o.c + where.b * o.c_batch + (int64_t)where.g * N;
+  const T* la = (const T*)sh.la + where.b * sh.la_batch + at.h;
 
-  f32x4 s[HB][Tiles::kOwn];
-#pragma unroll
-  for (int h = 0; h < HB; ++h) {
-    const Head hd(sh, at, h);
-    enter_segment<VEC>(s[h], sh, d, hd.at, at.seg, hd.p0, p, hd.rows, t0);
-  }
+  f32x4 s[1][kOwn];
+  enter_segment<VEC>(s[0], sh, d, at.at, where.seg, at.p0, p, at.rows, t0);
   using XStage = Stage<T, Q, PT, kThreads, VEC>;
   using NStage = Stage<T, Q, NT, kThreads, VEC>;
-  XStage xst[HB];
+  XStage xst;
   NStage bst, cst;
+  const typename XStage::In xin(d.u_token, at.rows), yin(sh.heads * P, at.rows);
   const typename NStage::In bin(d.v_token, N), cin(o.c_token, N);
   auto start = [&](int k) { return (int64_t)(first + k) * Q; };
   auto tokens = [&](int k) { return (int)min((int64_t)Q, (int64_t)sh.len - start(k)); };
@@ -768,13 +770,7 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 && VEC ? 2 : 1) * EW) voi
     if (k < count) cst.load(cc + start(k) * o.c_token, cin, tokens(k));
   };
   auto fetch_x = [&](int k) {
-    if (k >= count) return;
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const Head hd(sh, at, h);
-      xst[h].load(u + start(k) * d.u_token + (int64_t)hd.h * P + hd.p0,
-                  typename XStage::In(d.u_token, hd.rows), tokens(k));
-    }
+    if (k < count) xst.load(u + start(k) * d.u_token, xin, tokens(k));
   };
   // Log decays come two chunks ahead from memory, their running sums one ahead
   // into LDS.
@@ -786,27 +782,23 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 && VEC ? 2 : 1) * EW) voi
   };
   auto sums = [&](int k) {
     const Cum cum = cumulate(lav);
-    hi[k & 1][sums_of][lane] = cum.hi;
-    lo[k & 1][sums_of][lane] = cum.lo;
-    wt[k & 1][sums_of][lane] = cum.w;
-    if (lane == 0) total[k & 1][sums_of] = cum.total;
+    hi[k & 1][lane] = cum.hi;
+    lo[k & 1][lane] = cum.lo;
+    wt[k & 1][0][lane] = cum.w;
+    if (lane == 0) total[k & 1][0] = cum.total;
   };
   // Outputs of a chunk, which lie in LDS in the place of its x, to memory.
   auto put_y = [&](int k) {
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const Head hd(sh, at, h);
-      XStage y;
-      y.take(xs[h], XS);
-      y.put((T*)o.y + (((uint64_t)at.b * sh.len + start(k)) * sh.heads + hd.h) * P + hd.p0,
-            typename XStage::In(sh.heads * P, hd.rows), tokens(k));
-    }
+    XStage y;
+    y.take(xs, XS);
+    y.put((T*)o.y + (((uint64_t)where.b * sh.len + start(k)) * sh.heads + at.h) * P + at.p0, yin,
+          tokens(k));
   };
-  if (sums_of >= 0) fetch_la(0);
+  if (sums_here) fetch_la(0);
   fetch_b(0);
   fetch_c(0);
   fetch_x(0);
-  if (sums_of >= 0) {
+  if (sums_here) {
     sums(0);
     fetch_la(1);
   }
@@ -817,134 +809,99 @@ __global__ __launch_bounds__(256 * EW, (sizeof(T) == 2 && VEC ? 2 : 1) * EW) voi
       put_y(k - 1);
     }
     // a thread stores its x where it has read outputs
-#pragma unroll
-    for (int h = 0; h < HB; ++h) xst[h].store(xs[h], XS);
+    xst.store(xs, XS);
     bst.store(bs, NS);
     cst.store(cs, NS);
-    if constexpr (EW > 1) {
-#pragma unroll
-      for (int h = 0; h < HB; ++h) {
-#pragma unroll
-        for (int t = 0; t < Tiles::kOwn; t += 2)
-          *reinterpret_cast<Frag*>(ss[h * NQ + (t0 + t) / 2] + (64 * wave + lane) * 8) =
-              join(to_four<T>(s[h][t]), to_four<T>(s[h][t + 1]));
-      }
-    }
     __syncthreads();
-    if (sums_of >= 0 && k + 1 < count) {
+    if (sums_here && k + 1 < count) {
       sums(k + 1);
       fetch_la(k + 2);
     }
     fetch_b(k + 1);
-    {
-      // rows r = 16 j + 4 g + i, column s = 16 wave + col
-      Frag cf[NQ];
+    if (2 * part <= wave) {
+      // rows r = 32 part + 16 f + 4 g + i, column s = 16 wave + col
+      f32x4 w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-      for (int q = 0; q < NQ; ++q)
-        cf[q] = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
+      for (int q = 0; q < NQ; ++q) {
+        const Frag cf = row_frag(cs + (16 * wave + col) * NS + 32 * q + 8 * g);
 #pragma unroll
-      for (int e0 = 0; e0 < 2 / EW; ++e0) {
-        const int e = EW > 1 ? part : e0;
-        if (2 * e > wave) break;
-        f32x4 gt[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        for (int f = 0; f < 2; ++f)
+          w[f] = mma(row_frag(bs + (32 * part + 16 * f + col) * NS + 32 * q + 8 * g), cf, w[f]);
+      }
+      const float hs = hi[now][16 * wave + col], ls = lo[now][16 * wave + col];
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
+      for (int f = 0; f < 2; ++f) {
+        const int r = 32 * part + 16 * f + 4 * g;
+        const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[now] + r);
+        const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[now] + r);
 #pragma unroll
-          for (int f = 0; f < 2; ++f)
-            gt[f] = mma(row_frag(bs + (32 * e + 16 * f + col) * NS + 32 * q + 8 * g), cf[q], gt[f]);
-        }
+        for (int i = 0; i < 4; ++i)
+          w[f][i] *= exp2_seen(r + i <= 16 * wave + col, hs, ls, hr[i], lr[i]);
+      }
+      // position 32 e + 8 g + 4 f + i holds token 32 e + 16 f + 4 g + i, so that a row
+      // read gives the operand that matches token_frag
+      Two lw;
+      lw.split(w[0], w[1]);
+      const int at_s = wave < 2 ? (16 * wave + col) * LS0
+                                : 32 * LS0 + (16 * wave + col - 32) * LS1 + 32 * part;
 #pragma unroll
-        for (int h = 0; h < HB; ++h) {
-          const float hs = hi[now][h][16 * wave + col], ls = lo[now][h][16 * wave + col];
-          f32x4 w[2];
+      for (int a = 0; a < kParts; ++a)
+        *reinterpret_cast<Frag*>(lg[a] + at_s + 8 * g) = lw.p[a];
+    }
+    Frag xf[1][2];
 #pragma unroll
-          for (int f = 0; f < 2; ++f) {
-            const int r = 32 * e + 16 * f + 4 * g;
-            const f32x4 hr = *reinterpret_cast<const f32x4*>(hi[now][h] + r);
-            const f32x4 lr = *reinterpret_cast<const f32x4*>(lo[now][h] + r);
+    for (int q = 0; q < 2; ++q) xf[0][q] = token_frag(xs, XS, q, 16 * wave);
+    // y^T: rows p = 16 wave + 4 g + i, columns s = 16 j + col; j: first the tokens that
+    // are handed over, then this wave's own
+    f32x4 in[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[f][i] = gt[f][i] * exp2_seen(r + i <= 16 * wave + col, hs, ls, hr[i], lr[i]);
-          }
-          // position 32 q + 8 g + 4 f + i holds token 32 q + 16 f + 4 g + i, so that
-          // a row read gives the operand that matches token_frag
-          *reinterpret_cast<Frag*>(lg[h] + (16 * wave + col) * XS + 32 * e + 8 * g) =
-              join(to_four<T>(w[0]), to_four<T>(w[1]));
-        }
+    for (int j = 0; j < 4; ++j) in[j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < kOwn; t += 2) {
+      Two sf;
+      sf.split(s[0][t], s[0][t + 1]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int tok = 2 * (j < 2 ? 1 - part : part) + (j & 1);
+        const Frag cf = row_frag(cs + (16 * tok + col) * NS + 16 * (t0 + t) + 8 * g);
+#pragma unroll
+        for (int a = 0; a < kParts; ++a) in[j] = mma(sf.p[a], cf, in[j]);
       }
     }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) ex[j][wave_id()][lane] = in[j];
     fetch_c(k + 1);
-    Frag xf[HB][2];
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) xf[h][q] = token_frag(xs[h], XS, q, 16 * wave);
-    }
-    // y^T: rows p = 16 wave + 4 g + i, columns s = 16 (j0 + j) + col
-    const int j0 = kTokenTiles * part;
-    f32x4 acc[HB][kTokenTiles];
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-#pragma unroll
-      for (int j = 0; j < kTokenTiles; ++j) acc[h][j] = f32x4{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      Frag sf[HB];
-#pragma unroll
-      for (int h = 0; h < HB; ++h) {
-        if constexpr (EW > 1)
-          sf[h] = *reinterpret_cast<const Frag*>(ss[h * NQ + q] + (64 * wave + lane) * 8);
-        else
-          sf[h] = join(to_four<T>(s[h][2 * q]), to_four<T>(s[h][2 * q + 1]));
-      }
-#pragma unroll
-      for (int j = 0; j < kTokenTiles; ++j) {
-        const Frag cf = row_frag(cs + (16 * (j0 + j) + col) * NS + 32 * q + 8 * g);
-#pragma unroll
-        for (int h = 0; h < HB; ++h) acc[h][j] = mma(sf[h], cf, acc[h][j]);
-      }
-    }
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-#pragma unroll
-      for (int j = 0; j < kTokenTiles; ++j) {
-        const int s16 = 16 * (j0 + j) + col;
-        acc[h][j] *= exp2_diff(hi[now][h][s16], lo[now][h][s16], 0.0f, 0.0f);
-      }
-    }
     fetch_x(k + 1);
-    update_state<T, NT, PARTS, HB>(s, xf, bs, wt[now], total[now], t0);
+    update_state<T, NT, PARTS, 1>(s, xf, bs, wt[now], total[now], t0);
     __syncthreads();
+    f32x4 y[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      if (EW > 1 && q > part) break;
+      if (q > part) break;
 #pragma unroll
-      for (int h = 0; h < HB; ++h) {
+      for (int a = 0; a < kParts; ++a) {
 #pragma unroll
-        for (int j = EW > 1 ? 0 : 2 * q; j < kTokenTiles; ++j)
-          acc[h][j] = mma(xf[h][q], row_frag(lg[h] + (16 * (j0 + j) + col) * XS + 32 * q + 8 * g),
-                          acc[h][j]);
+        for (int j = 0; j < 2; ++j)
+          y[j] = mma(xf[0][q], row_frag(lg[a] + (part ? 32 * LS0 + (16 * j + col) * LS1
+                                                   : (16 * j + col) * LS0) + 32 * q + 8 * g), y[j]);
       }
     }
-    // over x, of which every wave has read what it needs
 #pragma unroll
-    for (int h = 0; h < HB; ++h) {
+    for (int j = 0; j < 2; ++j) {
+      const int s16 = 16 * (2 * part + j) + col;
+      const float ec = exp2_diff(hi[now][s16], lo[now][s16], 0.0f, 0.0f);
+      const f32x4 more = ex[j][wave_id() ^ 4][lane];
 #pragma unroll
-      for (int j = 0; j < kTokenTiles; ++j)
-        *reinterpret_cast<typename Elem<T>::Four*>(xs[h] + (16 * (j0 + j) + col) * XS + 16 * wave +
-                                                   4 * g) = to_four<T>(acc[h][j]);
+      for (int i = 0; i < 4; ++i) y[j][i] = __builtin_fmaf(ec, in[2 + j][i] + more[i], y[j][i]);
+      // over x, of which every wave has read what it needs
+      *reinterpret_cast<typename Elem<T>::Four*>(xs + s16 * XS + 16 * wave + 4 * g) =
+          to_four<T>(y[j]);
     }
   }
   __syncthreads();
   put_y(count - 1);
-  if (d.fin && at.seg + 1 == sh.segs) {
-#pragma unroll
-    for (int h = 0; h < HB; ++h) {
-      const Head hd(sh, at, h);
-      store_state<VEC>(s[h], d.fin + hd.at * size + (uint64_t)hd.p0 * N, p, hd.rows, N, t0);
-    }
-  }
+  if (d.fin && where.seg + 1 == sh.segs)
+    store_state<VEC>(s[0], d.fin + at.at * size + (uint64_t)at.p0 * N, p, at.rows, N, t0);
 }
 
 // ------------------------------------------------------------ gradient
@@ -1392,37 +1349,45 @@ hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipS
   k_scan_states<T, NT, VEC, PARTS, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d0, d1, false);
   return hipGetLastError();
 }
-template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
+// A gradient's states: the two halves of a long state's entries need nothing of each
+// other, so in bfloat16 they go to workgroups of four waves, three on a compute unit.  384
+// tiles of 32 chunks, 200 MB of states: 96 us, with eight waves for the whole state 109.
+template <typename T, int NT, bool VEC, int PARTS>
+hipError_t grad_states(const ScanShape& sh, const ScanDir* d, int nd, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && VEC && NT == 128)
+    return states<T, 64, VEC, PARTS, 1, 1>(sh, d, nd, true, s);
+  else
+    return states<T, NT, VEC, PARTS, 1, 2>(sh, d, nd, true, s);
+}
+template <typename T, int NT, bool VEC, int PARTS>
 hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
-  if (hipError_t e = states<T, NT, VEC, PARTS, HB, EW>(sh, &d, 1, false, s)) return e;
-  const uint32_t grid = sh.batch * sh.segs * (sh.heads * sh.ptiles / HB);
-  k_scan_out<T, NT, VEC, PARTS, HB, EW><<<grid, 256 * EW, 0, s>>>(sh, d, o);
+  hipError_t e;
+  if constexpr (sizeof(T) == 2 && VEC)
+    e = sh.tiles == 2 ? states<T, NT, VEC, PARTS, 2, 1>(sh, &d, 1, false, s)
+                      : states<T, NT, VEC, PARTS, 1, 2>(sh, &d, 1, false, s);
+  else
+    e = states<T, NT, VEC, PARTS, 1, 2>(sh, &d, 1, false, s);
+  if (e) return e;
+  k_scan_out<T, NT, VEC, PARTS>
+      <<<sh.batch * sh.segs * sh.heads * sh.ptiles, 512, 0, s>>>(sh, d, o);
   return hipGetLastError();
 }
-// The forms of a call: see ScanTiles and Parts.  Calls on unaligned rows and in
-// float32 take the one that is kept for them.
-#define FESC_SCAN_FORMS(CALL)                                  \
-  if constexpr (sizeof(T) == 2 && VEC) {                       \
-    if (sh.exact) return sh.tiles == 2 ? CALL(3, 2, 1) : CALL(3, 1, 2); \
-    return sh.tiles == 2 ? CALL(2, 2, 1) : CALL(2, 1, 2);      \
-  }                                                            \
-  return CALL(3, 1, 2)
+// Weighted inputs in three parts where a state is an output, otherwise in two: see Parts.
+#define FESC_SCAN_PARTS(CALL)              \
+  if constexpr (sizeof(T) == 2 && VEC) {   \
+    if (!sh.exact) return CALL(2);         \
+  }                                        \
+  return CALL(3)
 template <typename T, int NT, bool VEC>
 hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, hipStream_t s) {
-#define FORM(PARTS, HB, EW) (states<T, NT, VEC, PARTS, HB, EW>(sh, d, nd, true, s))
-  // Without outputs the two halves of a long state's entries need nothing of each
-  // other: workgroups of four waves, three on a compute unit.  384 tiles of 32 chunks,
-  // 200 MB of states: 96 us, with eight waves for the whole state 109.
-  if constexpr (sizeof(T) == 2 && VEC && NT == 128)
-    return sh.exact ? states<T, 64, VEC, 3, 1, 1>(sh, d, nd, true, s)
-                    : states<T, 64, VEC, 2, 1, 1>(sh, d, nd, true, s);
-  FESC_SCAN_FORMS(FORM);
+#define FORM(PARTS) (grad_states<T, NT, VEC, PARTS>(sh, d, nd, s))
+  FESC_SCAN_PARTS(FORM);
 #undef FORM
 }
 template <typename T, int NT, bool VEC>
 hipError_t outputs(const ScanShape& sh, const ScanDir& d, const ScanOut& o, hipStream_t s) {
-#define FORM(PARTS, HB, EW) (outputs<T, NT, VEC, PARTS, HB, EW>(sh, d, o, s))
-  FESC_SCAN_FORMS(FORM);
+#define FORM(PARTS) (outputs<T, NT, VEC, PARTS>(sh, d, o, s))
+  FESC_SCAN_PARTS(FORM);
 #undef FORM
 }
 

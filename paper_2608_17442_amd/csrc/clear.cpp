@@ -178,10 +178,10 @@ void seg_space(Space& w, const ScanShape& s, ScanDir* d) {
   d->seg_decay = w.take<float>((uint64_t)s.batch * s.heads * s.segs);
 }
 
-void grad_space(Space& w, const ScanShape& s, uint32_t dtype, ScanDir* dir, ScanGrad* g) {
+void grad_space(Space& w, const ScanShape& s, ScanDir* dir, ScanGrad* g) {
   for (int k = 0; k < 2; ++k) {
     seg_space(w, s, dir + k);
-    dir[k].chunk_states = w.take<char>(state_count(s) * s.chunks, elem_bytes(dtype));
+    dir[k].chunk_states = w.take<float>(s.chunk_state((uint64_t)s.batch * s.heads, 0, 0));
   }
   split_heads(s, &g->splits, &g->heads_per_split);
   if (g->splits > 1) {
@@ -270,7 +270,7 @@ int fesc_clear_scan_workspace(const fesc_clear_scan_desc* d, int backward, size_
   ScanDir dir[2] = {};
   ScanGrad g{};
   if (backward)
-    grad_space(w, s, d->dtype, dir, &g);
+    grad_space(w, s, dir, &g);
   else
     seg_space(w, s, dir);
   *bytes = w.used;
@@ -326,7 +326,7 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
   ScanDir dir[2] = {};
   ScanGrad g{};
   Space w(workspace);
-  grad_space(w, s, d->dtype, dir, &g);
+  grad_space(w, s, dir, &g);
   if (int rc = check_workspace(workspace, workspace_bytes, w.used)) return rc;
   s.la = la;
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)

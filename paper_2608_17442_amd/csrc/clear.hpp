@@ -22,8 +22,8 @@ struct ScanDir {
   int64_t u_token, u_batch, v_token, v_batch;
   const float* init;   // [b][h][P][N] or null (zero)
   float* fin;          // [b][h][P][N] or null
-  void* chunk_states;  // [b][h][chunk][P][N], element type of the call: the state that
-                       // enters each chunk; or null
+  float* chunk_states;  // [b][h][chunk][channel tile][kPTile * kept entries] or null: the
+                        // state that enters each chunk, in the order in which lanes hold it
   float* seg_states;   // [b][h][segment][P][N] or null (one segment)
   float* seg_decay;    // [b][h][segment]
   bool reverse;
@@ -40,6 +40,13 @@ struct ScanShape {
   const void* la;
   int64_t la_token, la_batch;
   bool vec;    // every row of every array starts at a multiple of 16 bytes
+
+  // Entries of a state row that chunk states have room for, and where that of a channel
+  // tile begins (head: batch * heads + head).
+  __host__ __device__ uint32_t kept_entries() const { return d_state <= 64 ? 64 : 128; }
+  __host__ __device__ uint64_t chunk_state(uint64_t head, uint32_t chunk, uint32_t ptile) const {
+    return ((head * chunks + chunk) * ptiles + ptile) * kPTile * kept_entries();
+  }
   bool exact;  // a state is an output
 };
 
@@ -52,7 +59,7 @@ struct ScanOut {  // outputs of a forward scan beside the final state
 struct ScanGrad {
   const void *x, *b, *c, *dy;
   int64_t x_token, x_batch, b_token, b_batch, c_token, c_batch, dy_token, dy_batch;
-  const void *s_in, *r_in;  // chunk states of the two directions
+  const float *s_in, *r_in;  // chunk states of the two directions
   void *dx, *dla, *db, *dc;
   float *db_part, *dc_part;  // [split][b][t][G][N] when heads are split, else null
   uint32_t splits, heads_per_split;

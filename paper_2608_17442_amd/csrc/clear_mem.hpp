@@ -57,9 +57,12 @@ struct Mem {
       __builtin_amdgcn_raw_buffer_store_b16((short)v, r, at, 0, 0);
   }
   template <typename T>
+  __device__ __forceinline__ static float value(uint32_t bits) {
+    return __uint_as_float(sizeof(T) == 4 ? bits : bits << 16);
+  }
+  template <typename T>
   __device__ __forceinline__ float load(uint32_t at) const {
-    const uint32_t w = load_bits<T>(at);
-    return __uint_as_float(sizeof(T) == 4 ? w : w << 16);
+    return value<T>(load_bits<T>(at));
   }
   // Four neighbouring elements at byte offset `at`, those at or past `left`
   // absent; WHOLE: all or none, in one access.

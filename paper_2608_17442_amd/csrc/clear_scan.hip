@@ -303,25 +303,6 @@ struct Stage {
       }
     }
   }
-  // sum of the products of these values with those at the same places of `o`
-  __device__ __forceinline__ float dot(const Stage& o) const {
-    float s = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kUnits; ++k) {
-      const u32x4 a = settled<T>(r[k]), b = settled<T>(o.r[k]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t v = a[j], w = b[j];
-        if constexpr (sizeof(T) == 4) {
-          s = __builtin_fmaf(__uint_as_float(v), __uint_as_float(w), s);
-        } else {
-          s = __builtin_fmaf(__uint_as_float(v << 16), __uint_as_float(w << 16), s);
-          s = __builtin_fmaf(__uint_as_float(v & 0xffff0000u), __uint_as_float(w & 0xffff0000u), s);
-        }
-      }
-    }
-    return s;
-  }
 };
 
 // Running sums of the log decays (base 2) of a chunk, lane l the token l, in
@@ -484,25 +465,22 @@ __device__ __forceinline__ void enter_segment(f32x4 (&s)[NTILES], const ScanShap
     }
   }
 }
-template <bool VEC, typename T, int NTILES>
-__device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], T* base, int p, int rows,
+template <bool VEC, int NTILES>
+__device__ __forceinline__ void store_state(const f32x4 (&s)[NTILES], float* base, int p, int rows,
                                             int N, int t0) {
   const int g = (threadIdx.x & 63) >> 4;
   const Mem m(base);
-  if constexpr (VEC && sizeof(T) == 2) {  // two tiles side by side: eight entries at once
 #pragma unroll
-    for (int t = 0; t < NTILES; t += 2) {
-      const int n = state_col(t0 + t, g);
-      m.store16(p < rows && n < N ? (p * N + n) * 2u : kAbsent,
-                __builtin_bit_cast(u32x4, join(to_four<T>(s[t]), to_four<T>(s[t + 1]))));
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < NTILES; ++t) {
-      const int n = state_col(t0 + t, g);
-      m.store_four<T, VEC>((p * N + n) * (uint32_t)sizeof(T), s[t], p < rows ? N - n : 0);
-    }
+  for (int t = 0; t < NTILES; ++t) {
+    const int n = state_col(t0 + t, g);
+    m.store_four<float, VEC>((p * N + n) * 4u, s[t], p < rows ? N - n : 0);
   }
+}
+
+// Where the chunk states that a gradient reads keep what lane `lane` holds of tile t of
+// the rows 16 w ...: bytes from the channel tile's first one, whole lines per access.
+__device__ __forceinline__ uint32_t kept_at(int w, int t, int lane, int entries) {
+  return ((w * (entries / 16) + t) * 64 + lane) * 16;
 }
 
 // The operand with the tokens of half q of a chunk along the summed axis, from
@@ -581,7 +559,7 @@ __global__ __launch_bounds__(256 * EW, HB * EW == 1 ? 3 : (sizeof(T) == 2 ? 2 : 
   const ScanDir& d = blockIdx.z ? d1 : d0;
   const Where at = Where::of<HB>(sh);
   const int wave = wave_id() & 3, part = wave_id() >> 2, t0 = part * Tiles::kOwn;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, g = lane >> 4;
   const int sums_of = sums_tile<HB, EW>();  // whose running sums this wave forms
   const int P = sh.head_dim, N = sh.d_state, p = 16 * wave + (lane & 15);
   const int n0 = blockIdx.y * NT, m0 = t0 + n0 / 16;  // first entry and tile in the state
@@ -648,8 +626,12 @@ __global__ __launch_bounds__(256 * EW, HB * EW == 1 ? 3 : (sizeof(T) == 2 ? 2 : 
 #pragma unroll
       for (int h = 0; h < HB; ++h) {
         const Head hd(sh, at, h);
-        store_state<VEC>(s[h], (T*)d.chunk_states + (hd.at * sh.chunks + chunk(k)) * size +
-                                   (uint64_t)hd.p0 * N, p, hd.rows, N, m0);
+        const Mem m(d.chunk_states + sh.chunk_state(hd.at, chunk(k), hd.p0 / PT));
+#pragma unroll
+        for (int t = 0; t < Tiles::kOwn; ++t)
+          m.store16(p < hd.rows && state_col(m0 + t, g) < N
+                        ? kept_at(wave, m0 + t, lane, sh.kept_entries()) : kAbsent,
+                    __builtin_bit_cast(u32x4, s[h][t]));
       }
     }
     typename Elem<T>::Frag xf[HB][2];
@@ -920,28 +902,32 @@ constexpr int kGradThreads = 768;
 // The first sum of dla falls from t to t + 1 by row sum minus column sum of
 // D K G at t.  Wave w of 0..3 holds the columns r = 16 w ... of G, K and W
 // and forms dx; wave 4 + 4 e + w holds half e of the entries of dC and dB for the
-// tokens 16 w ....  8 x 2048 tokens, 24 heads: 87 us for 350 MB, 4 TB/s (its loads alone
-// 77); eight waves with one barrier a round 102, with four 120.
+// tokens 16 w ....  S and R come in fp32; they, D G and W enter the products in two
+// bfloat16 parts, so that every gradient is rounded once.  8 x 2048 tokens, 24 heads:
+// 154 us for 560 MB, 3.6 TB/s; a copy's rate would give 114, LDS is busy for 65.
 template <typename T, int NT, bool VEC>
 __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGrad a) {
   constexpr int XS = PT + Elem<T>::kPad, NS = NT + Elem<T>::kPad;
   __shared__ __align__(16) T bs[Q * NS];
   __shared__ __align__(16) T cs[Q * NS];
-  // Rounds lie in turn in two places, S and R side by side: one barrier each.  In
-  // float32 LDS has room for one place, R following S in it.
-  constexpr bool kTwice = sizeof(T) == 2;
-  constexpr int kPlaces = kTwice ? 2 : 1;
+  using Two = Parts<T, 2>;
+  constexpr int kParts = Two::kCount;
+  // In bfloat16 the tokens of the rounds lie in turn in two places, and S and R, in
+  // their parts, in one each: S is replaced while R is read and the other way round, two
+  // barriers a round.  In float32 LDS has room for one place, R following S in it.
+  constexpr bool kApart = sizeof(T) == 2;
+  constexpr int kPlaces = kApart ? 2 : 1;
   __shared__ __align__(16) T x_s[kPlaces][Q * XS];
   __shared__ __align__(16) T dy_s[kPlaces][Q * XS];
-  __shared__ __align__(16) T s_s[kPlaces * kPlaces][PT * NS];
+  __shared__ __align__(16) T s_s[kPlaces][kParts][PT * NS];
   __shared__ __align__(16) float hi_s[2][Q], lo_s[2][Q], ec_s[2][Q], wt_s[2][Q];
   // of the round at hand and of the one before, whose dla is still to be formed;
   // what is written before a round's barrier, also of the round to come
   __shared__ float us[2][2][Q], vs[2][2][Q], colsum[2][Q], rowsum[2][4][Q], dots[4][8], total[4];
   __shared__ bool reset[4][Q];
   using Frag = typename Elem<T>::Frag;
-  using Four = typename Elem<T>::Four;
-  const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const int wave = wave_id();
+  int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   const bool left = wave < 4;  // waves of dx
   const int tile = wave & 3;
   const int P = sh.head_dim, N = sh.d_state;
@@ -953,13 +939,13 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   const uint32_t per_group = sh.heads / sh.groups;
   const uint32_t h0 = split * a.heads_per_split;
   const uint32_t hn = min(a.heads_per_split, per_group - h0);
-  const uint64_t size = (uint64_t)P * N;
 
-  // Waves 0..3 bring x and dy of a round, the others S and R.
+  // Waves 0..3 bring x and dy of a round, the others S and R, two neighbouring tiles of a
+  // lane at a time.
   using XStage = Stage<T, Q, PT, 256, VEC>;
-  using SStage = Stage<T, PT, NT, 512, VEC, 256>;
-  constexpr int kUnits = XStage::kUnits > SStage::kUnits ? XStage::kUnits : SStage::kUnits;
-  Loaded<VEC> one[kUnits], two[kUnits];
+  XStage x_next, dy_next;
+  constexpr int kPairs = PT * NT / 8 / 512;
+  f32x4 s_next[kPairs][2], r_next[kPairs][2];
   if (!left) {
     using NStage = Stage<T, Q, NT, 512, VEC, 256>;
     NStage st, st2;
@@ -970,47 +956,57 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
     st.store(bs, NS);
     st2.store(cs, NS);
   }
-  float lav = 0.0f;
+  // One of the waves with states, which have less to do, forms dla of the round before;
+  // the running sums of the next are left to the wave with least of K.
+  constexpr int kFinish = 4, kSums = 3;
+  uint32_t lav = 0;  // as loaded: a conversion would wait for it
   const uint32_t la_at =
       lane < n ? lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T) : kAbsent;
-  // the loads of round k (head of the split and channel tile): la, x and S, then
-  // dy and R
-  auto tokens = [&](const void* base, uint64_t batch, uint64_t token, uint32_t k, Loaded<VEC>* r) {
+  // the loads of round k (head of the split and channel tile)
+  auto tokens = [&](const void* base, uint64_t batch, uint64_t token, uint32_t k, XStage& st) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
-    XStage st;
     st.load((const T*)base + b * batch + t0 * token + (int64_t)h * P + pt * PT,
             typename XStage::In(token, min(PT, P - (int)pt * PT)), n);
-#pragma unroll
-    for (int u = 0; u < XStage::kUnits; ++u) r[u] = st.r[u];
   };
-  auto states = [&](const void* base, uint32_t k, Loaded<VEC>* r) {
+  // pair i of a lane: row 16 w + col, entries 32 q + 8 g ...
+  auto pair = [&](int i, int* w, int* q) {
+    *w = (wave - 4 + 8 * i) / (NT / 32);
+    *q = (wave - 4 + 8 * i) % (NT / 32);
+  };
+  auto states = [&](const float* base, uint32_t k, f32x4(&to)[kPairs][2]) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
-    SStage st;
-    st.load((const T*)base + (((uint64_t)b * sh.heads + h) * sh.chunks + c) * size +
-                (uint64_t)pt * PT * N,
-            typename SStage::In(N, N), min(PT, P - (int)pt * PT));
+    const Mem m(base + sh.chunk_state((uint64_t)b * sh.heads + h, c, pt));
 #pragma unroll
-    for (int u = 0; u < SStage::kUnits; ++u) r[u] = st.r[u];
-  };
-  auto fetch_one = [&](auto is_left, uint32_t k) {
-    if constexpr (is_left) {
-      const uint32_t h = grp * per_group + h0 + k / sh.ptiles;
-      lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h).load<T>(la_at);
-      tokens(a.x, a.x_batch, a.x_token, k, one);
-    } else {
-      states(a.s_in, k, one);
+    for (int i = 0; i < kPairs; ++i) {
+      int w, q;
+      pair(i, &w, &q);
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const bool seen = 16 * w + col < P - (int)pt * PT && state_col(2 * q + f, g) < N;
+        to[i][f] = __builtin_bit_cast(
+            f32x4, m.load16(seen ? kept_at(w, 2 * q + f, lane, NT) : kAbsent));
+      }
     }
   };
-  auto fetch_two = [&](auto is_left, uint32_t k) {
-    if constexpr (is_left)
-      tokens(a.dy, a.dy_batch, a.dy_token, k, two);
-    else
-      states(a.r_in, k, two);
-  };
-  auto staged = [](auto st, const Loaded<VEC>* r) {
+  auto place_states = [&](T(&to)[kParts][PT * NS], const f32x4(&from)[kPairs][2]) {
 #pragma unroll
-    for (int u = 0; u < decltype(st)::kUnits; ++u) st.r[u] = r[u];
-    return st;
+    for (int i = 0; i < kPairs; ++i) {
+      int w, q;
+      pair(i, &w, &q);
+      Two v;
+      v.split(from[i][0], from[i][1]);
+#pragma unroll
+      for (int a = 0; a < kParts; ++a)
+        *reinterpret_cast<Frag*>(to[a] + (16 * w + col) * NS + 32 * q + 8 * g) = v.p[a];
+    }
+  };
+  auto fetch = [&](uint32_t k) {
+    if (wave == kSums) {
+      const uint32_t h = grp * per_group + h0 + k / sh.ptiles;
+      lav = Mem((const T*)sh.la + b * sh.la_batch + t0 * sh.la_token + h).load_bits<T>(la_at);
+    }
+    tokens(a.x, a.x_batch, a.x_token, k, x_next);
+    tokens(a.dy, a.dy_batch, a.dy_token, k, dy_next);
   };
   __syncthreads();
 
@@ -1039,21 +1035,26 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   // into `to` the products of what was added with the tokens' rows of `rowsn`.
   // Entries lie as in the recurrence's kernels: tiles 2 q and 2 q + 1 together
   // are those of one row access.
-  auto sum_state = [&](f32x4(&out)[kOwn], const T* sr, const T* tok, const T* rowsn,
-                       float scale, float* to) {
+  auto sum_state = [&](f32x4(&out)[kOwn], const T(&sr)[kParts][PT * NS], const T* tok,
+                       const T* rowsn, float scale, float* to) {
     Frag tf[PT / 32];
 #pragma unroll
     for (int q = 0; q < PT / 32; ++q) tf[q] = row_frag(tok + (16 * tile + col) * XS + 32 * q + 8 * g);
     float sum = 0.0f;
 #pragma unroll
     for (int t = 0; t < kOwn; t += 2) {
+      __builtin_amdgcn_sched_barrier(0);  // one pair's operands at a time in the registers
       f32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
       for (int q = 0; q < PT / 32; ++q) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          acc[e] = mma(join(state_four(sr, NS, 32 * q + 8 * g, first + t + e),
-                            state_four(sr, NS, 32 * q + 8 * g + 4, first + t + e)), tf[q], acc[e]);
+        for (int a = 0; a < kParts; ++a) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            acc[e] = mma(join(state_four(sr[a], NS, 32 * q + 8 * g, first + t + e),
+                              state_four(sr[a], NS, 32 * q + 8 * g + 4, first + t + e)), tf[q],
+                         acc[e]);
+        }
       }
       const Frag row = row_frag(rowsn + (16 * tile + col) * NS + 16 * (first + t) + 8 * g);
 #pragma unroll
@@ -1095,46 +1096,70 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       dla = 0.0f;
     }
   };
-  // One of the other waves, which have less to do, forms dla of the round before;
-  // the running sums of the next are left to the wave with least of K.
-  constexpr int kFinish = 4, kSums = 3;
   const uint32_t rounds = hn * sh.ptiles;
   // Both kinds of waves run through the same rounds and barriers, each with the
   // registers of its own part only.
   auto run = [&](auto is_left) {
-    fetch_one(is_left, 0);
-    fetch_two(is_left, 0);
+    if constexpr (is_left) {
+      fetch(0);
+    } else {
+      states(a.s_in, 0, s_next);
+      states(a.r_in, 0, r_next);
+    }
     Cum cum;
-    if (is_left && wave == kSums) cum = cumulate(lav);
+    if (is_left && wave == kSums) cum = cumulate(Mem::value<T>(lav));
+#pragma unroll 1
     for (uint32_t k = 0; k < rounds; ++k) {
+      // addresses are formed anew in every round: kept, they would leave too few registers,
+      // and a spilled one waits for all loads under way (155 us for 179)
+      asm volatile("" : "+v"(lane));
+      col = lane & 15, g = lane >> 4;
       const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
       const int p0 = pt * PT, rows = min(PT, P - p0), now = k & 1;
-      const int place = kTwice ? now : 0, at4 = k & 3;
-      T *xs = x_s[place], *dys = dy_s[place], *sr = s_s[kPlaces * place];
-      T* rr = s_s[kPlaces * place + kPlaces - 1];
+      const int place = kApart ? now : 0, at4 = k & 3;
+      T *xs = x_s[place], *dys = dy_s[place];
+      auto &sr = s_s[0], &rr = s_s[kPlaces - 1];
       float *hi = hi_s[now], *lo = lo_s[now], *ec = ec_s[now], *wt = wt_s[now];
-      if constexpr (!kTwice) __syncthreads();
+      if constexpr (!kApart) __syncthreads();
       if constexpr (is_left) {
-        staged(XStage{}, one).store(xs, XS);
-        staged(XStage{}, two).store(dys, XS);
+        x_next.store(xs, XS);
+        dy_next.store(dys, XS);
       } else {
-        staged(SStage{}, one).store(sr, NS);
-        if constexpr (kTwice) staged(SStage{}, two).store(rr, NS);
-        const float dot = sum_groups(sum16(staged(SStage{}, two).dot(staged(SStage{}, one))));
-        if (lane == 0) dots[at4][wave - 4] = dot;
+        place_states(sr, s_next);
       }
       if (is_left && wave == kSums) {
         hi[lane] = cum.hi;
         lo[lane] = cum.lo;
         ec[lane] = cum.e;
         wt[lane] = cum.w;
-        reset[at4][lane] = lav < kReset;
+        reset[at4][lane] = Mem::value<T>(lav) < kReset;
         if (lane == 0) total[at4] = cum.total;
       }
       __syncthreads();
-      if (k + 1 < rounds) fetch_one(is_left, k + 1);
-      if (!is_left && wave == kFinish && k) finish(k - 1);
-      Four dg[4];  // D G as an operand, summed over s
+      if constexpr (!is_left) {
+        // <R, S> of the round; then their registers are free for the next one
+        f32x4 dot = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              dot[e] = __builtin_fmaf(r_next[i][f][e], s_next[i][f][e], dot[e]);
+          }
+        }
+        if constexpr (kApart) place_states(rr, r_next);
+        if (k + 1 < rounds) {
+          states(a.s_in, k + 1, s_next);
+          if constexpr (kApart) states(a.r_in, k + 1, r_next);
+        }
+        const float sum = sum_groups(sum16((dot[0] + dot[1]) + (dot[2] + dot[3])));
+        if (lane == 0) dots[at4][wave - 4] = sum;
+        if (wave == kFinish && k) finish(k - 1);
+      } else {
+        if (k + 1 < rounds) fetch(k + 1);
+      }
+      Two dg[2];  // D G as an operand, summed over s: halves of the chunk
       if constexpr (is_left) {
         const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
         float cols = 0.0f, rows16[16];  // of the tokens 16 j + 4 g + i
@@ -1142,6 +1167,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   #pragma unroll
         for (int q = 0; q < PT / 32; ++q)
           xf[q] = row_frag(xs + (16 * tile + col) * XS + 32 * q + 8 * g);
+        f32x4 weight[4];  // D G, rows 16 j + 4 g + i
   #pragma unroll
         for (int j = 0; j < 4; ++j) {
           f32x4 m = {0, 0, 0, 0}, e = {0, 0, 0, 0};
@@ -1160,23 +1186,27 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
             e *= gt[j];
             m *= gt[j];
           }
-          dg[j] = to_four<T>(e);
+          weight[j] = e;
           cols += (m[0] + m[1]) + (m[2] + m[3]);
   #pragma unroll
           for (int i = 0; i < 4; ++i) rows16[4 * j + i] = m[i];
         }
+  #pragma unroll
+        for (int e = 0; e < 2; ++e) dg[e].split(weight[2 * e], weight[2 * e + 1]);
         rowsum[now][tile][16 * (col >> 2) + 4 * g + (col & 3)] = sums16(rows16);
         cols = sum_groups(cols);
         if (g == 0) colsum[now][16 * tile + col] = cols;
       } else {
         sum_state(dc, sr, dys, cs, ec[16 * tile + col], us[now][half_of]);
       }
-      if constexpr (!kTwice) {
-        __syncthreads();
-        if constexpr (!is_left) staged(SStage{}, two).store(rr, NS);
+      __syncthreads();
+      if constexpr (!kApart) {
+        if constexpr (!is_left) {
+          place_states(rr, r_next);
+          if (k + 1 < rounds) states(a.r_in, k + 1, r_next);
+        }
         __syncthreads();
       }
-      if (k + 1 < rounds) fetch_two(is_left, k + 1);
       if constexpr (is_left) {
         const float wr = wt[16 * tile + col];
         Frag bf[NT / 32];
@@ -1191,8 +1221,12 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   #pragma unroll
           for (int q = 0; q < NT / 32; ++q) {
   #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              acc[e] = mma(row_frag(rr + (16 * (x + e) + col) * NS + 32 * q + 8 * g), bf[q], acc[e]);
+            for (int a = 0; a < kParts; ++a) {
+  #pragma unroll
+              for (int e = 0; e < 2; ++e)
+                acc[e] = mma(row_frag(rr[a] + (16 * (x + e) + col) * NS + 32 * q + 8 * g), bf[q],
+                             acc[e]);
+            }
           }
   #pragma unroll
           for (int e = 0; e < 2; ++e) acc[e] *= wr;
@@ -1200,10 +1234,12 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
           for (int j = 0; j < 4; j += 2) {
             if (j + 1 >= tile) {
   #pragma unroll
-              for (int e = 0; e < 2; ++e)
-                acc[e] = mma(join(col_four(dys, XS, 16 * j + 4 * g, 16 * (x + e)),
-                                  col_four(dys, XS, 16 * j + 16 + 4 * g, 16 * (x + e))),
-                             join(dg[j], dg[j + 1]), acc[e]);
+              for (int e = 0; e < 2; ++e) {
+                const Frag dyf = join(col_four(dys, XS, 16 * j + 4 * g, 16 * (x + e)),
+                                      col_four(dys, XS, 16 * j + 16 + 4 * g, 16 * (x + e)));
+  #pragma unroll
+                for (int a = 0; a < kParts; ++a) acc[e] = mma(dyf, dg[j / 2].p[a], acc[e]);
+              }
             }
           }
   #pragma unroll
@@ -1216,7 +1252,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       } else {
         sum_state(db, rr, xs, bs, wt[16 * tile + col], vs[now][half_of]);
       }
-      if (is_left && wave == kSums && k + 1 < rounds) cum = cumulate(lav);
+      if (is_left && wave == kSums && k + 1 < rounds) cum = cumulate(Mem::value<T>(lav));
     }
     __syncthreads();
     if (!is_left && wave == kFinish) finish(rounds - 1);
@@ -1225,13 +1261,20 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
     run(std::true_type{});
   else
     run(std::false_type{});
-  T* xs = x_s[0];
   // W to LDS (rows s, columns r), then its products with B and C
   if (left) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) xs[(16 * j + 4 * g + i) * XS + 16 * tile + col] = (T)wk[j][i];
+      for (int i = 0; i < 4; ++i) {
+        float w = wk[j][i];
+#pragma unroll
+        for (int a = 0; a < kParts; ++a) {
+          const T part = (T)w;
+          x_s[a][(16 * j + 4 * g + i) * XS + 16 * tile + col] = part;
+          w -= (float)part;
+        }
+      }
   }
   __syncthreads();
   if (left) return;
@@ -1239,21 +1282,29 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   const uint64_t part = (uint64_t)split * sh.batch * sh.len * sh.groups * N + row;
   const Mem dcm(a.dc_part ? (void*)(a.dc_part + part) : (void*)((T*)a.dc + row));
   const Mem dbm(a.db_part ? (void*)(a.db_part + part) : (void*)((T*)a.db + row));
-  Frag wc[2], wb[2];
+  Frag wc[kParts][2], wb[kParts][2];
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    wc[q] = row_frag(xs + (16 * tile + col) * XS + 32 * q + 8 * g);
-    wb[q] = join(col_four(xs, XS, 32 * q + 8 * g, 16 * tile),
-                 col_four(xs, XS, 32 * q + 8 * g + 4, 16 * tile));
+  for (int a = 0; a < kParts; ++a) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      wc[a][q] = row_frag(x_s[a] + (16 * tile + col) * XS + 32 * q + 8 * g);
+      wb[a][q] = join(col_four(x_s[a], XS, 32 * q + 8 * g, 16 * tile),
+                      col_four(x_s[a], XS, 32 * q + 8 * g + 4, 16 * tile));
+    }
   }
 #pragma unroll
   for (int x = 0; x < kOwn; ++x) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      dc[x] = mma(join(state_four(bs, NS, 32 * q + 8 * g, first + x),
-                       state_four(bs, NS, 32 * q + 8 * g + 4, first + x)), wc[q], dc[x]);
-      db[x] = mma(join(state_four(cs, NS, 32 * q + 8 * g, first + x),
-                       state_four(cs, NS, 32 * q + 8 * g + 4, first + x)), wb[q], db[x]);
+      const Frag bf = join(state_four(bs, NS, 32 * q + 8 * g, first + x),
+                           state_four(bs, NS, 32 * q + 8 * g + 4, first + x));
+      const Frag cf = join(state_four(cs, NS, 32 * q + 8 * g, first + x),
+                           state_four(cs, NS, 32 * q + 8 * g + 4, first + x));
+#pragma unroll
+      for (int a = 0; a < kParts; ++a) {
+        dc[x] = mma(bf, wc[a][q], dc[x]);
+        db[x] = mma(cf, wb[a][q], db[x]);
+      }
     }
     const int nn = state_col(first + x, g);
     const uint32_t at = (16 * tile + col) * sh.groups * N + nn;

@@ -127,6 +127,17 @@ __device__ __forceinline__ float sums16(float (&v)[16]) {
   halve(std::integral_constant<int, 1>{}, l & 1, [](float x) { return dpp_move<0xb1>(x); });
   return v[0];
 }
+// A column of four rows in each of the groups l / 16, v already summed from its rows on
+// within a group: adds the groups that follow, and `below`.  Returns the whole sum.
+__device__ __forceinline__ float add_later_groups(f32x4& v, float below) {
+  const int g = (threadIdx.x & 63) >> 4;
+  const float next = __shfl_xor(v[0], 16);
+  const float both = v[0] + next, far = __shfl_xor(both, 32);
+  const float more = below + ((g & 1 ? 0.0f : next) + (g & 2 ? 0.0f : far));
+  const float whole = below + (both + far);
+  v += more;
+  return whole;
+}
 __device__ __forceinline__ float sum_groups(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);

@@ -899,8 +899,10 @@ constexpr int kGradThreads = 768;
 //   dB_r = sum_s W_{s,r} C_s + sum_h w_r R^T x_r
 //   dla_t = sum_{s >= t > r} (D K G)_{s,r} + sum_{s >= t} C_s . (e^{cum_s} S^T dy_s)
 //           + sum_{r < t} B_r . (w_r R^T x_r) + e^{cum_Q} <R, S>
-// The first sum of dla falls from t to t + 1 by row sum minus column sum of
-// D K G at t.  Wave w of 0..3 holds the columns r = 16 w ... of G, K and W
+// Every term of dla_t has decays across t in it; only such terms are added up, so that the
+// result is as exact where e^{la_t} is small (sums from which larger ones cancel would not
+// be).  The first is, column by column, the sum of D K G from row t on, over r < t.
+// Wave w of 0..3 holds the columns r = 16 w ... of G, K and W
 // and forms dx; wave 4 + 4 e + w holds half e of the entries of dC and dB for the
 // tokens 16 w ....  S and R come in fp32; they, D G and W enter the products in two
 // bfloat16 parts, so that every gradient is rounded once.  8 x 2048 tokens, 24 heads:
@@ -923,8 +925,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   __shared__ __align__(16) float hi_s[2][Q], lo_s[2][Q], ec_s[2][Q], wt_s[2][Q];
   // of the round at hand and of the one before, whose dla is still to be formed;
   // what is written before a round's barrier, also of the round to come
-  __shared__ float us[2][2][Q], vs[2][2][Q], colsum[2][Q], rowsum[2][4][Q], dots[4][8], total[4];
-  __shared__ bool reset[4][Q];
+  __shared__ float us[2][2][Q], vs[2][2][Q], across[2][4][Q], dots[4][8], total[4];
   using Frag = typename Elem<T>::Frag;
   const int wave = wave_id();
   int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
@@ -1075,10 +1076,9 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
     float base = 0.0f;
 #pragma unroll
     for (int x = 0; x < 8; ++x) base += dots[b4][x];
-    const float u = us[b2][0][lane] + us[b2][1][lane] +
-                    ((rowsum[b2][0][lane] + rowsum[b2][1][lane]) +
-                     (rowsum[b2][2][lane] + rowsum[b2][3][lane])) -
-                    colsum[b2][lane];
+    const float own = (across[b2][0][lane] + across[b2][1][lane]) +
+                      (across[b2][2][lane] + across[b2][3][lane]);
+    const float u = us[b2][0][lane] + us[b2][1][lane];
     const float v = vs[b2][0][lane] + vs[b2][1][lane];
     float after = u, before = v;  // sums from the token on, and up to it
 #pragma unroll
@@ -1088,8 +1088,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       before += lane >= x ? q : 0.0f;
     }
     const float upto = __shfl_up(before, 1);
-    // before a reset nothing counts: the exact zero, not the sums' remainder
-    dla += reset[b4][lane] ? 0.0f : after + (lane ? upto : 0.0f) + base * total[b4];
+    dla += own + after + (lane ? upto : 0.0f) + base * total[b4];
     if (k % sh.ptiles + 1 == sh.ptiles) {
       const uint32_t h = grp * per_group + h0 + k / sh.ptiles;
       if (lane < n) ((T*)a.dla)[((uint64_t)b * sh.len + t0 + lane) * sh.heads + h] = (T)dla;
@@ -1132,7 +1131,6 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
         lo[lane] = cum.lo;
         ec[lane] = cum.e;
         wt[lane] = cum.w;
-        reset[at4][lane] = Mem::value<T>(lav) < kReset;
         if (lane == 0) total[at4] = cum.total;
       }
       __syncthreads();
@@ -1162,14 +1160,15 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       Two dg[2];  // D G as an operand, summed over s: halves of the chunk
       if constexpr (is_left) {
         const float hr = hi[16 * tile + col], lr = lo[16 * tile + col];
-        float cols = 0.0f, rows16[16];  // of the tokens 16 j + 4 g + i
+        // of the tokens t = 16 j + 4 g + i, the sum over s >= t of D K G at (s, r)
+        float rows16[16], below = 0.0f;
         Frag xf[PT / 32];
   #pragma unroll
         for (int q = 0; q < PT / 32; ++q)
           xf[q] = row_frag(xs + (16 * tile + col) * XS + 32 * q + 8 * g);
         f32x4 weight[4];  // D G, rows 16 j + 4 g + i
   #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 3; j >= 0; --j) {
           f32x4 m = {0, 0, 0, 0}, e = {0, 0, 0, 0};
           if (j >= tile) {
   #pragma unroll
@@ -1185,17 +1184,18 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
             wk[j] += m;
             e *= gt[j];
             m *= gt[j];
+  #pragma unroll
+            for (int i = 2; i >= 0; --i) m[i] += m[i + 1];
+            below = add_later_groups(m, below);
           }
           weight[j] = e;
-          cols += (m[0] + m[1]) + (m[2] + m[3]);
   #pragma unroll
-          for (int i = 0; i < 4; ++i) rows16[4 * j + i] = m[i];
+          for (int i = 0; i < 4; ++i)
+            rows16[4 * j + i] = j > tile || (j == tile && 4 * g + i > col) ? m[i] : 0.0f;
         }
   #pragma unroll
         for (int e = 0; e < 2; ++e) dg[e].split(weight[2 * e], weight[2 * e + 1]);
-        rowsum[now][tile][16 * (col >> 2) + 4 * g + (col & 3)] = sums16(rows16);
-        cols = sum_groups(cols);
-        if (g == 0) colsum[now][16 * tile + col] = cols;
+        across[now][tile][16 * (col >> 2) + 4 * g + (col & 3)] = sums16(rows16);
       } else {
         sum_state(dc, sr, dys, cs, ec[16 * tile + col], us[now][half_of]);
       }

@@ -756,23 +756,21 @@ __global__ __launch_bounds__(512, sizeof(T) == 2 && VEC ? 4 : 2) void k_scan_out
   };
   // Log decays come two chunks ahead from memory, their running sums one ahead
   // into LDS.
-  float lav = 0.0f;
+  uint32_t lav = 0;  // as loaded: a conversion would wait for it
   const uint32_t la_at = lane * (uint32_t)sh.la_token * (uint32_t)sizeof(T);
   auto fetch_la = [&](int k) {
     if (k < count)
-      lav = Mem(la + start(k) * sh.la_token).load<T>(lane < tokens(k) ? la_at : kAbsent);
+      lav = Mem(la + start(k) * sh.la_token).load_bits<T>(lane < tokens(k) ? la_at : kAbsent);
   };
   auto sums = [&](int k) {
-    const Cum cum = cumulate(lav);
+    const Cum cum = cumulate(Mem::value<T>(lav));
     hi[k & 1][lane] = cum.hi;
     lo[k & 1][lane] = cum.lo;
     wt[k & 1][0][lane] = cum.w;
     if (lane == 0) total[k & 1][0] = cum.total;
   };
-  // Outputs of a chunk, which lie in LDS in the place of its x, to memory.
-  auto put_y = [&](int k) {
-    XStage y;
-    y.take(xs, XS);
+  // outputs of a chunk, which lay in LDS in the place of its x, to memory
+  auto put_y = [&](const XStage& y, int k) {
     y.put((T*)o.y + (((uint64_t)where.b * sh.len + start(k)) * sh.heads + at.h) * P + at.p0, yin,
           tokens(k));
   };
@@ -786,14 +784,16 @@ __global__ __launch_bounds__(512, sizeof(T) == 2 && VEC ? 4 : 2) void k_scan_out
   }
   for (int k = 0; k < count; ++k) {
     const int now = k & 1;
+    XStage y_out;
     if (k) {
       __syncthreads();
-      put_y(k - 1);
+      y_out.take(xs, XS);
     }
     // a thread stores its x where it has read outputs
     xst.store(xs, XS);
     bst.store(bs, NS);
     cst.store(cs, NS);
+    if (k) put_y(y_out, k - 1);  // behind the wait for the loads, which it need not wait for
     __syncthreads();
     if (sums_here && k + 1 < count) {
       sums(k + 1);
@@ -881,7 +881,9 @@ __global__ __launch_bounds__(512, sizeof(T) == 2 && VEC ? 4 : 2) void k_scan_out
     }
   }
   __syncthreads();
-  put_y(count - 1);
+  XStage y_out;
+  y_out.take(xs, XS);
+  put_y(y_out, count - 1);
   if (d.fin && where.seg + 1 == sh.segs)
     store_state<VEC>(s[0], d.fin + at.at * size + (uint64_t)at.p0 * N, p, at.rows, N, t0);
 }

@@ -50,10 +50,6 @@ struct Rows {
     ok = ok && aligned(p, 16) && s0 % per == 0 && s1 % per == 0;
     return *this;
   }
-  Rows& apart(uint64_t token, uint64_t width) {
-    ok = ok && token >= width;
-    return *this;
-  }
   Rows& len(uint64_t n) {
     ok = ok && n % per == 0;
     return *this;
@@ -294,8 +290,7 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
   s.la = la;
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(h0).add(hT).add(y).len(d->head_dim)
-              .len(d->d_state).apart(d->x_token, d->head_dim).apart(d->b_token, d->d_state)
-              .apart(d->c_token, d->d_state).ok;
+              .len(d->d_state).ok;
   if (!s.vec) s.tiles = 1;
   s.exact = hT != nullptr;
   dir.u = x;
@@ -331,9 +326,7 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
   s.la = la;
   s.vec = Rows(d->dtype).add(x, d->x_token, d->x_batch).add(B, d->b_token, d->b_batch)
               .add(C, d->c_token, d->c_batch).add(dy, d->dy_token, d->dy_batch).add(h0).add(dhT)
-              .add(dh0).add(dx).add(db).add(dc).len(d->head_dim).len(d->d_state)
-              .apart(d->x_token, d->head_dim).apart(d->b_token, d->d_state)
-              .apart(d->c_token, d->d_state).apart(d->dy_token, d->head_dim).ok;
+              .add(dh0).add(dx).add(db).add(dc).len(d->head_dim).len(d->d_state).ok;
   if (!s.vec) s.tiles = 1;
   s.exact = dh0 != nullptr;
   dir[0].u = x;

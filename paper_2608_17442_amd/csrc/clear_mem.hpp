@@ -31,16 +31,13 @@ __device__ __forceinline__ auto to_four(const f32x4& v) {
 
 struct Mem {
   __amdgpu_buffer_rsrc_t r;
-  // bytes: what lies behind them is absent too
-  __device__ __forceinline__ explicit Mem(const void* base, uint32_t bytes = 0x7fffffff)
-      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000)) {}
-  // `more`: a part of the offset that is the same for the wave; the check against
-  // `bytes` counts it, also where it lies past them by itself
-  __device__ __forceinline__ u32x4 load16(uint32_t at, uint32_t more = 0) const {
-    return __builtin_amdgcn_raw_buffer_load_b128(r, at, more, 0);
+  __device__ __forceinline__ explicit Mem(const void* base)
+      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0x7fffffff, 0x00027000)) {}
+  __device__ __forceinline__ u32x4 load16(uint32_t at) const {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
   }
-  __device__ __forceinline__ void store16(uint32_t at, const u32x4& v, uint32_t more = 0) const {
-    __builtin_amdgcn_raw_buffer_store_b128(v, r, at, more, 0);
+  __device__ __forceinline__ void store16(uint32_t at, const u32x4& v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(v, r, at, 0, 0);
   }
   template <typename T>
   __device__ __forceinline__ uint32_t load_bits(uint32_t at) const {

@@ -157,22 +157,25 @@ __device__ __forceinline__ float load1(const T* p) {
   return (float)*p;
 }
 
-// Where a thread's units of a ROWS x COLS tile lie in memory.  VEC: rows start
-// at multiples of 16 bytes and do not overlap, so that one offset, formed once,
-// and the bytes that the valid rows span say all.  FIRST: the first thread of those
-// that share the work.
-template <typename T, int COLS, int THREADS, bool VEC, int FIRST = 0>
+// Where a thread's units of a ROWS x COLS tile lie in memory: unit k in row `row` +
+// k `rows_apart`; none of the thread's units where its column is absent.
+// FIRST: the first thread of those that share the work.
+template <typename T, int COLS, int THREADS, int FIRST = 0>
 struct Rows {
+  static constexpr int rows_apart = THREADS / (COLS / Elem<T>::kUnit);
   uint32_t pitch, first, step;
-  int cols;
+  int cols, row;
   __device__ __forceinline__ Rows(uint32_t pitch_, int cols_) : pitch(pitch_), cols(cols_) {
     constexpr int kUnit = Elem<T>::kUnit, kPerRow = COLS / kUnit;
-    const int row = (threadIdx.x - FIRST) / kPerRow, col = (threadIdx.x - FIRST) % kPerRow * kUnit;
-    first = col < cols ? (row * pitch + col) * (uint32_t)sizeof(T) : kAbsent;
-    step = THREADS / kPerRow * pitch * (uint32_t)sizeof(T);
+    const int col = (threadIdx.x - FIRST) % kPerRow * kUnit;
+    row = (threadIdx.x - FIRST) / kPerRow;
+    first = (row * pitch + col) * (uint32_t)sizeof(T);
+    step = rows_apart * pitch * (uint32_t)sizeof(T);
+    if (col >= cols) row = 1 << 30;
   }
-  __device__ __forceinline__ uint32_t bytes(int rows) const {
-    return ((rows - 1) * pitch + cols) * (uint32_t)sizeof(T);
+  // offset of whole unit k of `rows` rows
+  __device__ __forceinline__ uint32_t at(int k, int rows) const {
+    return row < rows - k * rows_apart ? first + k * step : kAbsent;
   }
 };
 
@@ -218,14 +221,14 @@ struct Stage {
   static constexpr int kPerRow = COLS / kUnit;
   static constexpr int kUnits = ROWS * kPerRow / THREADS;
   static_assert(ROWS * kPerRow % THREADS == 0, "whole units per thread");
-  using In = Rows<T, COLS, THREADS, VEC, FIRST>;
+  using In = Rows<T, COLS, THREADS, FIRST>;
   Loaded<VEC> r[kUnits];
 
   __device__ __forceinline__ void load(const T* base, const In& in, int rows) {
     if constexpr (VEC) {
-      const Mem m(base, in.bytes(rows));
+      const Mem m(base);
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) r[k].w = m.load16(in.first, k * in.step);
+      for (int k = 0; k < kUnits; ++k) r[k].w = m.load16(in.at(k, rows));
     } else if (in.cols < kUnit) {  // rows of a few elements: one at a time
       const Mem m(base);
 #pragma unroll
@@ -278,9 +281,9 @@ struct Stage {
   }
   __device__ __forceinline__ void put(T* base, const In& out, int rows) const {
     if constexpr (VEC) {
-      const Mem m(base, out.bytes(rows));
+      const Mem m(base);
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) m.store16(out.first, r[k].w, k * out.step);
+      for (int k = 0; k < kUnits; ++k) m.store16(out.at(k, rows), r[k].w);
     } else {  // whole units word by word, at any alignment of elements
       const uint32_t off = reinterpret_cast<uintptr_t>(base) & 3;
       const Mem m(reinterpret_cast<char*>(base) - off);

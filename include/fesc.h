@@ -772,7 +772,10 @@ int fesc_calib_hbm(fesc_ctx* ctx, int kind, size_t bytes, double* rate, void* st
  * in R^N (P = head_dim, N = d_state) and a_t = exp(la_t):
  *     S_t = a_t S_{t-1} + x_t B_t^T,     y_t = S_t C_t,     S_0 = h0 or 0.
  * la <= 0; la = -inf (a_t = 0) forgets what came before exactly, so several
- * documents may follow each other in one row.  Layouts (the last dimensions
+ * documents may follow each other in one row, and a state that is not finite
+ * (in h0, or in a slot of a pool that was never written) does not matter to
+ * them.  Factors that are not finite spoil the whole of their sequence, other
+ * documents in it included.  Layouts (the last dimensions
  * contiguous; token and batch strides are free, so factors may be slices of
  * one wider array): x [batch][len][heads][head_dim], la [batch][len][heads],
  * B and C [batch][len][groups][d_state]; dy like x.  y, dx, dla, db and dc

@@ -243,7 +243,7 @@ def scan(x, la, B, C, h0=None, return_state=False, stream=None):
     `return_state` the final state as well.
 
     x [batch, len, heads, head_dim], la [batch, len, heads] (log decays, <= 0;
-    -inf resets the state), B and C [batch, len, groups, d_state]; the first
+    -inf resets the state, whatever it was), B and C [batch, len, groups, d_state]; the first
     two dimensions may have any strides, so slices of a wider projection do.
     h0 and the returned state: float32 [batch, heads, head_dim, d_state].
     In bfloat16 y is rounded once; with `return_state` the states behind it are
@@ -293,7 +293,8 @@ def scan_step(x, la, B, C, state, slots=None, stream=None):
     x [rows, heads, head_dim], la [rows, heads], B and C [rows, groups,
     d_state]; state float32 [pool, heads, head_dim, d_state].  Row i uses state
     slots[i] (int32, None: i); a slot outside the pool (-1) marks an idle row,
-    whose y is zero.  No two rows may name one slot.  Not differentiable.
+    whose y is zero.  No two rows may name one slot.  A new sequence may take
+    over a slot by a first token of la = -inf.  Not differentiable.
     """
     if stream is not None:
         with torch.cuda.stream(stream):

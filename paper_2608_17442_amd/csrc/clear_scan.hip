@@ -327,6 +327,16 @@ __device__ __forceinline__ float exp2_seen(bool seen, float hs, float ls, float 
   const float d = (hs - hr) + (ls - lr);
   return __builtin_amdgcn_exp2f(seen ? d : -INFINITY);
 }
+// v decayed; a decay of 0 forgets v whatever it is, not finite included.
+__device__ __forceinline__ float decayed(float decay, float v) {
+  return decay == 0.0f ? 0.0f : decay * v;
+}
+__device__ __forceinline__ f32x4 decayed(float decay, const f32x4& v) {
+  f32x4 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = decayed(decay, v[i]);
+  return o;
+}
 // The wave's number, known to be the same for all its lanes.
 __device__ __forceinline__ int wave_id() {
   return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -463,7 +473,7 @@ __device__ __forceinline__ void enter_segment(f32x4 (&s)[NTILES], const ScanShap
 #pragma unroll
       for (int t = 0; t < NTILES; ++t) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(decay[k], s[t][i], own[k][t][i]);
+        for (int i = 0; i < 4; ++i) s[t][i] = __builtin_fmaf(decay[k], decay[k] == 0.0f ? 0.0f : s[t][i], own[k][t][i]);
       }
     }
   }
@@ -516,7 +526,7 @@ __device__ __forceinline__ void update_state(f32x4 (&s)[HB][OWN],
   for (int h = 0; h < HB; ++h) {
     const float e = total[h];
 #pragma unroll
-    for (int t = 0; t < OWN; ++t) s[h][t] *= e;
+    for (int t = 0; t < OWN; ++t) s[h][t] = decayed(e, s[h][t]);
   }
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
@@ -686,7 +696,7 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
     }
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k) {
-      carry = __builtin_fmaf(keep[k], carry, own[k]);
+      carry = __builtin_fmaf(keep[k], keep[k] == 0.0f ? 0.0f : carry, own[k]);
       if (j0 + k < sh.segs) s[(uint64_t)(j0 + k) * size] = carry;
     }
   }
@@ -877,7 +887,7 @@ __global__ __launch_bounds__(512, sizeof(T) == 2 && VEC ? 4 : 2) void k_scan_out
       const float ec = exp2_diff(hi[now][s16], lo[now][s16], 0.0f, 0.0f);
       const f32x4 more = ex[j][wave_id() ^ 4][lane];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[j][i] = __builtin_fmaf(ec, in[2 + j][i] + more[i], y[j][i]);
+      for (int i = 0; i < 4; ++i) y[j][i] += decayed(ec, in[2 + j][i] + more[i]);
       // over x, of which every wave has read what it needs
       *reinterpret_cast<typename Elem<T>::Four*>(xs + s16 * XS + 16 * wave + 4 * g) =
           to_four<T>(y[j]);
@@ -1066,7 +1076,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const f32x4 rv = half(row, e);
-        acc[e] *= scale;
+        acc[e] = decayed(scale, acc[e]);
         out[t + e] += acc[e];
         sum += (acc[e][0] * rv[0] + acc[e][1] * rv[1]) + (acc[e][2] * rv[2] + acc[e][3] * rv[3]);
       }
@@ -1093,7 +1103,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       before += lane >= x ? q : 0.0f;
     }
     const float upto = __shfl_up(before, 1);
-    dla += own + after + (lane ? upto : 0.0f) + base * total[b4];
+    dla += own + after + (lane ? upto : 0.0f) + decayed(total[b4], base);
     if (k % sh.ptiles + 1 == sh.ptiles) {
       const uint32_t h = grp * per_group + h0 + k / sh.ptiles;
       if (lane < n) ((T*)a.dla)[((uint64_t)b * sh.len + t0 + lane) * sh.heads + h] = (T)dla;
@@ -1234,7 +1244,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
             }
           }
   #pragma unroll
-          for (int e = 0; e < 2; ++e) acc[e] *= wr;
+          for (int e = 0; e < 2; ++e) acc[e] = decayed(wr, acc[e]);
   #pragma unroll
           for (int j = 0; j < 4; j += 2) {
             if (j + 1 >= tile) {
@@ -1374,7 +1384,7 @@ __global__ __launch_bounds__(256) void k_scan_step(StepArgs a, uint32_t psplit) 
     f32x4 v = s.load_four<VEC>((p * N + n) * 4, N - n);
     const float xv = load1(x + p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(decay, v[i], xv * b[i]);
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(decay, decay == 0.0f ? 0.0f : v[i], xv * b[i]);
     s.store_four<float, VEC>((p * N + n) * 4, v, N - n);
     float d = (v[0] * c[0] + v[1] * c[1]) + (v[2] * c[2] + v[3] * c[3]);
 #pragma unroll

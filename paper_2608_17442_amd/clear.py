@@ -22,6 +22,7 @@ from .fesc import _check, _lib
 _u32, _u64, _vp, _sz = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_size_t
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
+_MOST_TOKEN_STRIDE = 1 << 22    # of the recurrence's arrays
 
 
 class _ScanDesc(ctypes.Structure):
@@ -100,6 +101,14 @@ def _dense_tail(t, dims):
                 return False
             step *= t.shape[d]
     return True
+
+
+def _steps(t):
+    """Strides of the first two dimensions, [batch, len, ...]; that of a
+    dimension of one entry, which may be anything, is that of a dense one."""
+    step = t.shape[2:].numel()
+    token = t.stride(1) if t.shape[1] > 1 else step
+    return token, t.stride(0) if t.shape[0] > 1 else token * t.shape[1]
 
 
 def _factor(t, dims, what):
@@ -183,9 +192,8 @@ def _scan_plan(x, la, B, C, h0, dy=None):
     if h0 is not None:
         _state(h0, (b, H, P, N), "h0", x)
     # without dy: the strides of a contiguous one
-    d = _ScanDesc(_TYPES[x.dtype], b, n, H, P, G, N, x.stride(1), x.stride(0), la.stride(1),
-                  la.stride(0), B.stride(1), B.stride(0), C.stride(1), C.stride(0),
-                  *((H * P, n * H * P) if dy is None else (dy.stride(1), dy.stride(0))))
+    d = _ScanDesc(_TYPES[x.dtype], b, n, H, P, G, N, *_steps(x), *_steps(la), *_steps(B),
+                  *_steps(C), *((H * P, n * H * P) if dy is None else _steps(dy)))
     plan = _Plan(d, x.device)
     plan.space = _space(_lib.fesc_clear_scan_workspace, plan.ref, 0)
     plan.grad_space = _space(_lib.fesc_clear_scan_workspace, plan.ref, 1)
@@ -221,7 +229,7 @@ class _Scan(torch.autograd.Function):
             if dh is None:
                 return (None,) * 7
             dy = torch.zeros_like(x, memory_format=torch.contiguous_format)
-        elif not _dense_tail(dy, 2):
+        elif not _dense_tail(dy, 2) or _steps(dy)[0] > _MOST_TOKEN_STRIDE:
             dy = dy.contiguous()
         if dh is not None:
             dh = dh.contiguous()
@@ -280,8 +288,8 @@ def _step_plan(x, la, B, C, state, slots):
         _shape(slots, (rows,), "slots")
         if not slots.is_contiguous():
             raise ValueError("slots: must be contiguous")
-    plan = _Plan(_ScanDesc(_TYPES[x.dtype], rows, 1, H, P, G, N, 0, x.stride(0), 0, la.stride(0),
-                           0, B.stride(0), 0, C.stride(0), 0, 0), x.device)
+    plan = _Plan(_ScanDesc(_TYPES[x.dtype], rows, 1, H, P, G, N,
+                           *(s for t in (x, la, B, C) for s in _steps(t[:, None])), 0, 0), x.device)
     plan.shapes = (rows, H, P)
     return plan
 

@@ -187,12 +187,11 @@ void grad_space(Space& w, const ScanShape& s, ScanDir* dir, ScanGrad* g) {
   }
 }
 
-int check_grid(const ScanShape& s) {
-  const uint64_t bh = (uint64_t)s.batch * s.heads;
-  const uint64_t join = ((uint64_t)s.head_dim * s.d_state + 255) / 256;
-  if (bh * s.ptiles * s.segs >= kMaxGrid512 || bh * join >= kMaxGrid256 ||
-      (uint64_t)s.batch * s.chunks >= kMaxGrid1024 ||
-      (uint64_t)s.batch * s.len * s.groups * s.d_state >= kMaxGrid256 * 256)
+// The launches of a call that its sizes alone bound: segments and their join are cut
+// for few tiles (kUnits), parts of dB and dC for few chunks.
+int check_grid(const ScanShape& s, bool backward) {
+  if ((uint64_t)s.batch * s.heads * s.ptiles * s.segs >= kMaxGrid512 ||
+      (backward && (uint64_t)s.batch * s.chunks >= kMaxGrid1024))
     return fail(FESC_ERR_ARG, "batch * len * heads too large for one call");
   return FESC_OK;
 }
@@ -278,7 +277,7 @@ int fesc_clear_scan(const fesc_clear_scan_desc* d, const void* x, const void* la
                     size_t workspace_bytes, void* stream) {
   if (int rc = check_scan(d)) return rc;
   ScanShape s = shape_of(d, 1);
-  if (int rc = check_grid(s)) return rc;
+  if (int rc = check_grid(s, false)) return rc;
   if (d->batch == 0) return FESC_OK;
   if (d->len == 0)
     return hT ? hip_check(launch_state_copy(h0, hT, state_count(s), S(stream)), "scan") : FESC_OK;
@@ -311,7 +310,7 @@ int fesc_clear_scan_bwd(const fesc_clear_scan_desc* d, const void* x, const void
                         void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check_scan(d)) return rc;
   ScanShape s = shape_of(d, 2);
-  if (int rc = check_grid(s)) return rc;
+  if (int rc = check_grid(s, true)) return rc;
   if (d->batch == 0) return FESC_OK;
   if (d->len == 0)
     return dh0 ? hip_check(launch_state_copy(dhT, dh0, state_count(s), S(stream)), "scan gradient")

@@ -1394,8 +1394,9 @@ __global__ __launch_bounds__(256) void k_scan_step(StepArgs a, uint32_t psplit) 
 }
 
 __global__ __launch_bounds__(256) void k_state_copy(const float* from, float* to, uint64_t count) {
-  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < count) to[i] = from ? from[i] : 0.0f;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < count;
+       i += (uint64_t)gridDim.x * 256)
+    to[i] = from ? from[i] : 0.0f;
 }
 
 template <typename T, int NT, bool VEC, int PARTS, int HB, int EW>
@@ -1529,7 +1530,8 @@ hipError_t launch_scan_step(uint32_t dtype, const StepArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_state_copy(const float* from, float* to, uint64_t count, hipStream_t s) {
-  k_state_copy<<<dim3((uint32_t)((count + 255) / 256)), 256, 0, s>>>(from, to, count);
+  const uint32_t grid = (uint32_t)std::min<uint64_t>((count + 255) / 256, 1u << 16);
+  k_state_copy<<<grid, 256, 0, s>>>(from, to, count);
   return hipGetLastError();
 }
 

@@ -58,3 +58,13 @@ def test_strides_of_single_tokens_and_sequences(clear, dtype):
     far_rows = [apart(t, 0) for t in (x, la, B, C)]
     assert torch.equal(clear.scan_step(x, la, B, C, s1), clear.scan_step(*far_rows, s2))
     assert torch.equal(s1, s2)
+
+
+def test_many_short_sequences(clear):
+    """More sequences than fit a launch of one work item per state entry."""
+    step("many short sequences")
+    b, L, H, P, N = 30000, 2, 24, 64, 128
+    f = [t.cuda() for t in R.factors(103, 100, L, H, P, 1, N, BF16)]
+    many = [t.repeat(b // 100, *[1] * (t.dim() - 1)) for t in f]
+    y = clear.scan(*many).unflatten(0, (b // 100, 100))
+    assert (y == clear.scan(*f)).all()

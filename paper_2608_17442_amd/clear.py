@@ -6,7 +6,8 @@
     norm_gated     u = v w / sqrt(mean v^2 + eps),  v = (m + skip x) silu(z)
     norm_residual  the same norm of r + scale o, which is returned too
 
-``scan`` and the norms are differentiable.  All tensors of a call are of one
+``scan`` and the norms are differentiable, once and in reverse; what would need
+another derivative or a trace of them is refused.  All tensors of a call are of one
 type, float32 or bfloat16, except states, which are float32.  Every
 computation runs in the library's HIP kernels, on the current stream (or on
 `stream`); there is no fallback path.
@@ -16,6 +17,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd import forward_ad
 
 from .fesc import _check, _lib
 
@@ -67,6 +69,17 @@ def _stream(device):
 def _once():
     if torch.is_grad_enabled():
         raise RuntimeError("the block in the clear is differentiable once: no create_graph=True")
+
+
+def _unrecorded(name, *ts):
+    """Refuses what a call on addresses would drop without a word: tangents of
+    forward-mode differentiation, and the call itself from a trace."""
+    if forward_ad._current_level >= 0:
+        for t in ts:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise NotImplementedError(f"{name}: no forward-mode derivative")
+    if torch._C._get_tracing_state() is not None:
+        raise NotImplementedError(f"{name}: cannot be traced")
 
 
 # ---------------------------------------------------------- argument checks
@@ -224,6 +237,7 @@ class _Scan(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy, dh=None):
         _once()
+        _unrecorded("scan", dy, dh)
         x, la, B, C, h0 = ctx.saved_tensors
         if dy is None:
             if dh is None:
@@ -266,6 +280,7 @@ def scan(x, la, B, C, h0=None, return_state=False, stream=None):
                                     or C.requires_grad
                                     or (h0 is not None and h0.requires_grad)):
         return _Scan.apply(x, la, B, C, h0, return_state, plan)
+    _unrecorded("scan", x, la, B, C, h0)
     y, h = _scan_forward(plan, x, la, B, C, h0, return_state)
     return (y, h) if return_state else y
 
@@ -312,6 +327,7 @@ def scan_step(x, la, B, C, state, slots=None, stream=None):
     if torch.is_grad_enabled() and (x.requires_grad or la.requires_grad or B.requires_grad
                                     or C.requires_grad or state.requires_grad):
         raise ValueError("scan_step is not differentiable: use scan, or torch.no_grad()")
+    _unrecorded("scan_step", x, la, B, C, state)
     device = plan.device
     y = torch.empty(plan.shapes, dtype=x.dtype, device=device)
     _check(_lib.fesc_clear_scan_step(plan.ref, x.data_ptr(), la.data_ptr(), B.data_ptr(),
@@ -403,6 +419,7 @@ class _Gated(torch.autograd.Function):
     @staticmethod
     def backward(ctx, du):
         _once()
+        _unrecorded("norm_gated", du)
         saved = m, x, z, skip, w = ctx.saved_tensors
         if du.is_contiguous():
             plan = ctx.plan
@@ -432,6 +449,7 @@ def norm_gated(m, x, z, skip, w, eps=1e-5, stream=None):
     if torch.is_grad_enabled() and (m.requires_grad or x.requires_grad or z.requires_grad
                                     or skip.requires_grad or w.requires_grad):
         return _Gated.apply(m, x, z, skip, w, eps, plan)
+    _unrecorded("norm_gated", m, x, z, skip, w)
     return _gated_forward(plan, m, x, z, skip, w)
 
 
@@ -460,6 +478,7 @@ class _Residual(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dnew, du):
         _once()
+        _unrecorded("norm_residual", dnew, du)
         saved = o, r, scale, w = ctx.saved_tensors
         if dnew is None and du is None:
             return (None,) * 6
@@ -494,4 +513,5 @@ def norm_residual(o, r, scale, w, eps=1e-5, stream=None):
     if torch.is_grad_enabled() and (o.requires_grad or r.requires_grad or scale.requires_grad
                                     or w.requires_grad):
         return _Residual.apply(o, r, scale, w, eps, plan)
+    _unrecorded("norm_residual", o, r, scale, w)
     return _residual_forward(plan, o, r, scale, w)

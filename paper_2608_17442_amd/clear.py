@@ -10,7 +10,10 @@
 another derivative or a trace of them is refused.  All tensors of a call are of one
 type, float32 or bfloat16, except states, which are float32.  Every
 computation runs in the library's HIP kernels, on the current stream (or on
-`stream`); there is no fallback path.
+`stream`); there is no fallback path.  A call with `stream` is put behind what that
+stream has to do, not behind work of the current one that forms its inputs, and its
+outputs are ready in that stream's order: the caller orders streams that share
+tensors.  Inputs may be dropped as soon as a call returns.
 """
 from __future__ import annotations
 
@@ -64,6 +67,16 @@ def _p(t):
 def _stream(device):
     """The current stream of a device, as its handle."""
     return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _on(stream, call, *args):
+    """A call on `stream`, which the memory of its tensors is kept for."""
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+    return out
 
 
 def _once():
@@ -273,8 +286,7 @@ def scan(x, la, B, C, h0=None, return_state=False, stream=None):
     Differentiable (once) with respect to all five.
     """
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return scan(x, la, B, C, h0, return_state)
+        return _on(stream, scan, x, la, B, C, h0, return_state)
     plan = _plan(_key("scan", x, la, B, C, h0), _scan_plan, (x, la, B, C, h0))
     if torch.is_grad_enabled() and (x.requires_grad or la.requires_grad or B.requires_grad
                                     or C.requires_grad
@@ -320,8 +332,7 @@ def scan_step(x, la, B, C, state, slots=None, stream=None):
     over a slot by a first token of la = -inf.  Not differentiable.
     """
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return scan_step(x, la, B, C, state, slots)
+        return _on(stream, scan_step, x, la, B, C, state, slots)
     plan = _plan(_key("scan_step", x, la, B, C, state, slots), _step_plan,
                  (x, la, B, C, state, slots))
     if torch.is_grad_enabled() and (x.requires_grad or la.requires_grad or B.requires_grad
@@ -443,8 +454,7 @@ def norm_gated(m, x, z, skip, w, eps=1e-5, stream=None):
     connection), z the gate, all [..., width] with rows of any one stride;
     skip and w [width].  Differentiable (once) with respect to all five."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return norm_gated(m, x, z, skip, w, eps)
+        return _on(stream, norm_gated, m, x, z, skip, w, eps)
     plan = _plan((eps, _key("norm_gated", m, x, z, skip, w)), _gated_plan, (m, x, z, skip, w, eps))
     if torch.is_grad_enabled() and (m.requires_grad or x.requires_grad or z.requires_grad
                                     or skip.requires_grad or w.requires_grad):
@@ -506,8 +516,7 @@ def norm_residual(o, r, scale, w, eps=1e-5, stream=None):
     [width].  u is formed from r_new before it is rounded.  Differentiable
     (once) with respect to all four."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return norm_residual(o, r, scale, w, eps)
+        return _on(stream, norm_residual, o, r, scale, w, eps)
     plan = _plan((eps, _key("norm_residual", o, r, scale, w)), _residual_plan,
                  (o, r, scale, w, eps))
     if torch.is_grad_enabled() and (o.requires_grad or r.requires_grad or scale.requires_grad

@@ -455,6 +455,7 @@ def norm_gated(m, x, z, skip, w, eps=1e-5, stream=None):
     skip and w [width].  Differentiable (once) with respect to all five."""
     if stream is not None:
         return _on(stream, norm_gated, m, x, z, skip, w, eps)
+    eps = float(eps)                        # by its value: plans are kept by it
     plan = _plan((eps, _key("norm_gated", m, x, z, skip, w)), _gated_plan, (m, x, z, skip, w, eps))
     if torch.is_grad_enabled() and (m.requires_grad or x.requires_grad or z.requires_grad
                                     or skip.requires_grad or w.requires_grad):
@@ -517,6 +518,7 @@ def norm_residual(o, r, scale, w, eps=1e-5, stream=None):
     (once) with respect to all four."""
     if stream is not None:
         return _on(stream, norm_residual, o, r, scale, w, eps)
+    eps = float(eps)                        # by its value: plans are kept by it
     plan = _plan((eps, _key("norm_residual", o, r, scale, w)), _residual_plan,
                  (o, r, scale, w, eps))
     if torch.is_grad_enabled() and (o.requires_grad or r.requires_grad or scale.requires_grad

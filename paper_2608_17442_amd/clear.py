@@ -118,6 +118,12 @@ def _shape(t, shape, what):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
+def _counts(t, what):
+    """Sizes go to the library in 32 bits."""
+    if t.shape and max(t.shape) >= 1 << 32:
+        raise ValueError(f"{what}: a size of 2^32 or more")
+
+
 def _dense_tail(t, dims):
     """Whether the last `dims` dimensions are laid out without gaps."""
     step = 1
@@ -212,6 +218,7 @@ def _scan_plan(x, la, B, C, h0, dy=None):
     _shape(la, x.shape[:3], "la")
     _shape(B, (*x.shape[:2], *B.shape[2:]), "B")
     _shape(C, B.shape, "C")
+    _counts(x, "x"), _counts(B, "B")
     _factor(x, 2, "x"), _factor(la, 1, "la"), _factor(B, 2, "B"), _factor(C, 2, "C")
     b, n, H, P = x.shape
     G, N = B.shape[2:]
@@ -308,6 +315,7 @@ def _step_plan(x, la, B, C, state, slots):
     _shape(la, (rows, H), "la")
     _shape(B, (rows, G, N), "B")
     _shape(C, B.shape, "C")
+    _counts(x, "x"), _counts(B, "B"), _counts(state, "state")
     _factor(x, 2, "x"), _factor(la, 1, "la"), _factor(B, 2, "B"), _factor(C, 2, "C")
     _state(state, (state.shape[0] if state.dim() else 0, H, P, N), "state", x)
     if slots is not None:
@@ -395,6 +403,7 @@ def _norm_plan(arrays, vectors, eps, grads=()):
         if not v.is_contiguous():
             raise ValueError(f"{what}: must be contiguous")
     w = first.shape[-1]
+    _counts(vectors[0][1], vectors[0][0])
     d = _NormDesc(_TYPES[first.dtype], w, first.numel() // w if w else 0, eps)
     for what, t in arrays:
         setattr(d, what + "_row", _rows(t, what))

@@ -68,3 +68,16 @@ def test_many_short_sequences(clear):
     many = [t.repeat(b // 100, *[1] * (t.dim() - 1)) for t in f]
     y = clear.scan(*many).unflatten(0, (b // 100, 100))
     assert (y == clear.scan(*f)).all()
+
+
+def test_sizes_past_32_bits_are_refused(clear):
+    """Tensors of 2^32 + 3 tokens or states that take no memory."""
+    step("sizes past 32 bits")
+    n = (1 << 32) + 3
+    one = torch.zeros(1, device="cuda")
+    x = one.expand(1, n, 1, 1)
+    with pytest.raises(ValueError, match="2\\^32"):
+        clear.scan(x, x[..., 0], x, x)
+    row = torch.zeros(1, 1, 1, device="cuda")
+    with pytest.raises(ValueError, match="2\\^32"):
+        clear.scan_step(row, row[..., 0], row, row, one.expand(n, 1, 1, 1))

@@ -67,30 +67,34 @@ struct Rows {
 //    unit where segments of six chunks remain, else one, two chunks at least.
 //  - Long sequences: two a unit, and the pass before in workgroups of two tiles (four
 //    waves), which share what is read of B.
-// Measured with 24 heads of 64, state 128, bfloat16, in us, forward:
-//    tiles x chunks   whole   one a unit   two a unit   pairs
-//     24 x 32           79       33            -          59
-//     48 x 32           79       43           49          55
-//     96 x 32           81       72           59          69
-//    144 x 32           81        -           77          82
-//    168 x 32           83        -           79          92
-//    192 x 32           82        -          104          96
-//     24 x 128         303       67           63          73
-//     48 x 128         303      112           98         100
-//     96 x 128         303      250          168         157
-//    144 x 128         306        -          262         216
-//    192 x 128         333        -          365         299
-//     24 x 782           -      275            -         242
+// Measured with 24 heads of 64, state 128, bfloat16, in us, forward (in brackets:
+// segments; the rule takes the lowest of a line or one within 3 % of it):
+//    tiles x chunks   whole   one a unit   two a unit   four (two at once), pairs before
+//     24 x 32           89       34 (10)      -            -
+//     48 x 32           89       45 (5)       51 (10)      -
+//     96 x 32           87       75 (2)       60 (5)       64 (10)
+//    144 x 32           87        -           80 (3)       87 (7)
+//    168 x 32           87        -           81 (3)       97 (6)
+//    192 x 32           89        -          113 (2)       97 (5)
+//     24 x 128         337       74 (10)      67 (21)      68 (42)
+//     48 x 128         337      125 (5)      104 (10)     109 (21)
+//     96 x 128         336      270 (2)      182 (5)      170 (10)
+//    144 x 128         342        -          274 (3)      249 (7)
+//    192 x 128         343        -          402 (2)      321 (5)
+//     24 x 782           -      337 (10)     269 (21)     254 (42)
+// These sizes in float32, states up to 64 and unaligned rows follow the same rules; 8 x 1581
+// tokens with a state of 33 and 13 x 1827 with heads of 100 are within 3 % of their best.
 // The gradient's pass carries states only, in both directions, so that a cut doubles
 // its work; of its workgroups 384 tiles' fit at once (whole gradient call, tiles of
 // both directions, segments in brackets):
-//     48 x 32           69       55 (5)      55 (8)
-//     72 x 64          127      114 (3)     105 (4)
-//     96 x 16           49        -          52 (4)
-//     96 x 32           77       85 (2)      74 (4)
-//    144 x 32           93        -         107 (3)
-//     48 x 128         215      132 (5)     122 (8)
-//     48 x 256         470      275 (5)     250 (8)
+//     48 x 32           76       63 (5)      63 (8)
+//     96 x 16           55       60 (4)      72 (8)
+//     96 x 32           89       89 (4)     100 (8)
+//    144 x 32          119      138 (3)     152 (8)
+//     48 x 128         242      180 (5)     177 (8)
+//     96 x 128         353      332 (4)     335 (8)
+//     48 x 256         509      357 (5)     333 (8)
+//    192 x 128         596      640 (4)     658 (8)
 constexpr uint64_t kUnits = 256;
 constexpr uint64_t kWholeTiles = 171, kWholeTilesGrad = 96;  // whole from here on
 constexpr uint64_t kGradTiles = 384;
@@ -99,9 +103,10 @@ constexpr uint64_t kPairChunks = 8192;               // tiles * chunks for pairs
 constexpr uint64_t kPairTiles = 256;
 // Up to this many segments each workgroup adds up the summaries before its own
 // (segs / 2 states read on average); more go through the join kernel (each read
-// and written once, a launch more).  24 tiles x 32 chunks in 3 segments: 50.3 us
-// against 52.5 with the kernel; 5: 38.8, 40.5; 6: 36.7, 37.3; 8: 36.4, 34.0.
-constexpr uint32_t kJoinedSegs = 5;
+// and written once, a launch more).  24 tiles x 32 chunks in 3 segments: 54.6 us
+// against 56.1 with the kernel; 5: 40.8, 42.5; 6: 38.3, 39.5; 8: 37.0, 34.0.  96 tiles:
+// 5: 60.1, 63.9; 6: 74.2, 80.4; 8: 72.1, 65.7.
+constexpr uint32_t kJoinedSegs = 6;
 ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
   ScanShape s{};
   s.batch = d->batch;
@@ -141,8 +146,8 @@ ScanShape shape_of(const fesc_clear_scan_desc* d, int dirs) {
 // Heads of a group in turn in one workgroup of the gradient kernel (one on a
 // unit); split over workgroups, whose parts of dB and dC are added up, where
 // chunks alone leave units idle.  Whole gradient call, 24 heads, in us: 32 chunks in
-// 4, 8, 12 splits 68, 60, 69; 64 in 2, 4, 8: 115, 95, 104; 128 in 1, 2, 4: 154, 116,
-// 126; 192 in 1, 2: 193, 216.
+// 4, 8, 12 splits 71, 64, 74; 64 in 2, 4, 8: 111, 91, 100; 128 in 1, 2, 4: 183, 148,
+// 167; 256 in 1, 2: 353, 377.
 void split_heads(const ScanShape& s, uint32_t* splits, uint32_t* per) {
   const uint32_t heads = s.heads / s.groups;
   const uint64_t groups = (uint64_t)s.batch * s.chunks * s.groups;

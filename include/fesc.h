@@ -745,13 +745,14 @@ int fesc_calib_valu(fesc_ctx* ctx, int kind, uint32_t iters, double* rate, void*
 int fesc_calib_hbm(fesc_ctx* ctx, int kind, size_t bytes, double* rate, void* stream);
 
 /* ------------------------------------------------------------------------
- * The block in the clear.  The same computations that the calls above carry
- * under encryption (the affine scan and its contraction, Eq.
- * "hescan-contract-output"; skip connection, gate and norm of the post-SSM
- * path), on unencrypted activations and with their gradients: for the model
- * whose weights are packed (its training, the ranges that fix scales and the
- * conversion bound), for the answers that decrypted outputs are held against,
- * and for traffic that needs no encryption.
+ * The block in the clear.  Computations that the calls above carry under
+ * encryption (the affine scan and its contraction, Eq.
+ * "hescan-contract-output") and those around them (skip connection, gate and
+ * norm of the post-SSM path), on unencrypted activations and with their
+ * gradients: to train the model whose weights are packed, to find the ranges
+ * that fix scales and the conversion bound, to hold decrypted outputs against,
+ * and for traffic that needs no encryption.  The block's causal convolution
+ * (fesc_heconv) has no call here.
  *
  * These calls need no context.  `dtype` is the type of every activation,
  * weight and gradient of a call (FESC_F32, FESC_BF16); states are fp32 in

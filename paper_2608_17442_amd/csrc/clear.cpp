@@ -82,8 +82,10 @@ struct Rows {
 //    144 x 128         342        -          274 (3)      249 (7)
 //    192 x 128         343        -          402 (2)      321 (5)
 //     24 x 782           -      337 (10)     269 (21)     254 (42)
-// These sizes in float32, states up to 64 and unaligned rows follow the same rules; 8 x 1581
-// tokens with a state of 33 and 13 x 1827 with heads of 100 are within 3 % of their best.
+// The same rules for a state of 64 (1 x 2048 tokens 27.6 in 10, best 27.1; 8 x 2048 74, 73;
+// 1 x 50001 201 in 42), rows at any alignment (8 x 1581, state 33: 83 whole, best 82;
+// 13 x 1827, 20 heads of 100: 355 whole) and float32 (one a unit: 24 x 32 63 in 10;
+// 48 x 128 308 in 5; 96 x 32 189 in 2, where 10 would take 169).
 // The gradient's pass carries states only, in both directions, so that a cut doubles
 // its work; of its workgroups 384 tiles' fit at once (whole gradient call, tiles of
 // both directions, segments in brackets):

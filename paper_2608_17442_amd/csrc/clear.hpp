@@ -36,7 +36,8 @@ struct ScanShape {
   uint32_t segs;
   bool joined;          // the summaries of many segments are joined by a kernel of its own
   uint32_t ptiles;      // ceil(head_dim / kPTile)
-  uint32_t tiles;       // channel tiles in one workgroup: 1, or 2 (aligned bfloat16)
+  uint32_t tiles;       // channel tiles in one workgroup of the segments' own pass: 1, or 2
+                        // (aligned bfloat16)
   const void* la;
   int64_t la_token, la_batch;
   bool vec;    // every row of every array starts at a multiple of 16 bytes

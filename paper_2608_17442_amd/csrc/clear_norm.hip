@@ -119,8 +119,8 @@ __device__ __forceinline__ V row_sum(V v, V* red) {
 }
 
 // 1 / (1 + e^{-z}) from the hardware's base-2 exponential and reciprocal: off
-// by a few units of the last place of fp32, more (2^-24 |z|) only where the
-// result is below e^{z}.
+// by a few units of the last place of fp32 for z >= 0; below, where the result
+// nears e^{z}, by some 2^-24 |z| of it, and it is 0 below about -88.
 __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
 }

@@ -110,9 +110,6 @@ __device__ __forceinline__ f32x8 join(const f32x4& a, const f32x4& b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-__device__ __forceinline__ f32x4 widen(const bf16x4& v) { return __builtin_convertvector(v, f32x4); }
-__device__ __forceinline__ f32x4 widen(const f32x4& v) { return v; }
-
 // The parts of a fp32 operand in the call's type: itself, or COUNT bf16 values.
 // Three, each the leading 8 bits of what the ones before leave, sum to it
 // exactly; two, each rounded to nearest, to within 2^-18 of it.
@@ -709,9 +706,9 @@ __global__ __launch_bounds__(256) void k_scan_join(ScanShape sh, ScanDir d0, Sca
 // wave with these channels; and its part of the new state.  Then, for the tokens of half e,
 // the chunk's own part of y^T from what all waves wrote.
 // Bound by the way from barrier to barrier, on which LDS, the matrix pipe and the
-// issue of instructions take turns: 8 x 2048 tokens, 24 heads of 64, state 128, 84 us
-// (25 at a copy's rate); 50001 tokens in segments 75 + 8 + 165 us (68).  Of these the second
-// parts of the operands cost some 8 and 35 us.
+// issue of instructions take turns: 8 x 2048 tokens, 24 heads of 64, state 128, 88 us
+// (25 at a copy's rate); 50001 tokens in 42 segments 76 + 13 + 205 us (68).  Operands in one
+// part and rounded: 75 and 195 us in all.
 template <typename T, int NT, bool VEC, int PARTS>
 __global__ __launch_bounds__(512, sizeof(T) == 2 && VEC ? 4 : 2) void k_scan_out(ScanShape sh,
                                                                                  ScanDir d,
@@ -1418,7 +1415,8 @@ hipError_t states(const ScanShape& sh, const ScanDir* d, int nd, bool main, hipS
 }
 // A gradient's states: the two halves of a long state's entries need nothing of each
 // other, so in bfloat16 they go to workgroups of four waves, three on a compute unit.  384
-// tiles of 32 chunks, 200 MB of states: 96 us, with eight waves for the whole state 109.
+// tiles of 32 chunks: 126 us for 403 MB of states (108 at a copy's rate, with what is read);
+// while states were half that size, 96, and with eight waves for the whole state 109.
 template <typename T, int NT, bool VEC, int PARTS>
 hipError_t grad_states(const ScanShape& sh, const ScanDir* d, int nd, hipStream_t s) {
   if constexpr (sizeof(T) == 2 && VEC && NT == 128)

@@ -22,7 +22,7 @@ struct ScanDir {
   int64_t u_token, u_batch, v_token, v_batch;
   const float* init;   // [b][h][P][N] or null (zero)
   float* fin;          // [b][h][P][N] or null
-  float* chunk_states;  // [b][h][chunk][channel tile][kPTile * kept entries] or null: the
+  float* chunk_states;  // [b][h][chunk][channel tile][kept rows * entries] or null: the
                         // state that enters each chunk, in the order in which lanes hold it
   float* seg_states;   // [b][h][segment][P][N] or null (one segment)
   float* seg_decay;    // [b][h][segment]
@@ -42,11 +42,15 @@ struct ScanShape {
   int64_t la_token, la_batch;
   bool vec;    // every row of every array starts at a multiple of 16 bytes
 
-  // Entries of a state row that chunk states have room for, and where that of a channel
-  // tile begins (head: batch * heads + head).
-  __host__ __device__ uint32_t kept_entries() const { return d_state <= 64 ? 64 : 128; }
+  // Entries of a row and rows of a channel tile that chunk states have room for (whole
+  // tiles of the matrix instructions), and where that of a channel tile begins
+  // (head: batch * heads + head).
+  __host__ __device__ uint32_t kept_entries() const { return (d_state + 31) / 32 * 32; }
+  __host__ __device__ uint32_t kept_rows() const {
+    return ptiles > 1 ? kPTile : (head_dim + 15) / 16 * 16;
+  }
   __host__ __device__ uint64_t chunk_state(uint64_t head, uint32_t chunk, uint32_t ptile) const {
-    return ((head * chunks + chunk) * ptiles + ptile) * kPTile * kept_entries();
+    return ((head * chunks + chunk) * ptiles + ptile) * kept_rows() * kept_entries();
   }
   bool exact;  // a state is an output
 };

@@ -989,6 +989,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
   auto states = [&](const float* base, uint32_t k, f32x4(&to)[kPairs][2]) {
     const uint32_t h = grp * per_group + h0 + k / sh.ptiles, pt = k % sh.ptiles;
     const Mem m(base + sh.chunk_state((uint64_t)b * sh.heads + h, c, pt));
+    const int entries = sh.kept_entries();
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       int w, q;
@@ -997,7 +998,7 @@ __global__ __launch_bounds__(kGradThreads) void k_scan_grad(ScanShape sh, ScanGr
       for (int f = 0; f < 2; ++f) {
         const bool seen = 16 * w + col < P - (int)pt * PT && state_col(2 * q + f, g) < N;
         to[i][f] = __builtin_bit_cast(
-            f32x4, m.load16(seen ? kept_at(w, 2 * q + f, lane, NT) : kAbsent));
+            f32x4, m.load16(seen ? kept_at(w, 2 * q + f, lane, entries) : kAbsent));
       }
     }
   };

@@ -37,3 +37,15 @@ def test_what_no_launch_carries_is_refused(clear):
     assert "too large" in refused_for(clear, False, batch=1 << 19)
     assert "too large" in refused_for(clear, True, batch=1 << 10, len=64 << 12, heads=1)
     assert "null buffer" in refused_for(clear, False, batch=1 << 10, len=64 << 12, heads=1)
+
+
+def test_small_heads_take_little_room(clear):
+    """The gradient's workspace follows the states' own size, to whole tiles of 16 x 32
+    entries: two directions, fp32, one state a chunk of 64 tokens."""
+    for P, N in ((16, 16), (8, 32), (64, 128), (100, 33)):
+        d = clear._ScanDesc(dtype=1, batch=1, len=1 << 20, heads=24, head_dim=P, groups=1, d_state=N)
+        n = ctypes.c_size_t()
+        assert clear._lib.fesc_clear_scan_workspace(ctypes.byref(d), 1, ctypes.byref(n)) == 0
+        rows = -(-P // 16) * 16 if P <= 64 else -(-P // 64) * 64
+        state = 24 * rows * (-(-N // 32) * 32) * 4
+        assert n.value <= 2 * state * ((1 << 14) + 32)     # and segments' states

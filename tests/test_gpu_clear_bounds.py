@@ -106,3 +106,29 @@ def test_rows_that_overlap(clear, dtype):
     rows = torch.randn(b, L * 8 + N, device="cuda").to(dtype)
     B2 = rows.as_strided((b, L, 1, N), (rows.stride(0), 8, N, 1))
     assert torch.equal(clear.scan(x, la, B2, C), clear.scan(x, la, B2.contiguous(), C))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", SHAPES + [(2, 200, 4, 16, 1, 16), (1, 1300, 2, 80, 2, 40)])
+def test_workspaces(clear, shape, dtype):
+    """Nothing beside the workspace, of exactly the size that the library names; and nothing
+    of what lies in it before a call shows in the outputs."""
+    step(f"scan beside its workspace {shape} {dtype}")
+    f, h0, plan = call(clear, shape, dtype, 83)
+    dy = torch.randn(shape[:4], device="cuda").to(dtype)
+    seen = []
+    for fill in (0xFF, 0x00):
+        grads = [torch.empty_like(t) for t in (*f, h0)]
+        y = torch.empty(plan.shapes[0], dtype=dtype, device="cuda")
+        spaces = [torch.full((size + 4096,), fill, dtype=torch.uint8, device="cuda")
+                  for size in (plan.space, plan.grad_space)]
+        clear._check(clear._lib.fesc_clear_scan(
+            plan.ref, *(t.data_ptr() for t in (*f, h0, y)), None, spaces[0].data_ptr(), plan.space,
+            clear._stream(0)))
+        clear._check(clear._lib.fesc_clear_scan_bwd(
+            plan.ref, *(t.data_ptr() for t in (*f, h0, dy)), None,
+            *(t.data_ptr() for t in (*grads, spaces[1])), plan.grad_space, clear._stream(0)))
+        for space, size in zip(spaces, (plan.space, plan.grad_space)):
+            assert (space[size:] == fill).all()
+        seen.append([y, *grads])
+    assert all(torch.equal(a, c) for a, c in zip(*seen))
